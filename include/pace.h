@@ -534,6 +534,79 @@ PACE_API size_t pace_token_logprob_backward_workspace_size(int64_t n_rows, int64
                                                            int32_t vocab_size);
 
 /* ------------------------------------------------------------------------ */
+/* Log-probabilities, entropy and alternatives from logits in memory         */
+/* ------------------------------------------------------------------------ */
+
+typedef enum { PACE_F32 = 0, PACE_BF16 = 1, PACE_F16 = 2 } pace_dtype;
+
+/* Logits z[n_rows][vocab_size] that are in memory: a rollout engine's decode
+ * step, or a head that pace_token_logprob does not cover.
+ *   logits      device, of `dtype`, aligned to its element; row r starts at
+ *               logits + r * row_stride (elements, >= vocab_size).
+ *   allowed     device uint32, or NULL (every place): bit j % 32 of word
+ *               allowed[r * allowed_stride + j / 32] is 1 where place j of row r
+ *               may be taken.  A place that is not allowed, or whose logit is
+ *               -inf, is excluded: it is outside every sum, whatever it holds.
+ *   mask        device uint8 [n_rows] or NULL (all rows): rows with 0 are not
+ *               read; their outputs are 0 (top_ids -1, top_logprob -inf).
+ *   vocab_size  1..2^24; n_rows up to 2^28. */
+typedef struct {
+  const void* logits;
+  int32_t dtype;          /* pace_dtype */
+  int32_t vocab_size;
+  int64_t n_rows;
+  int64_t row_stride;
+  const uint32_t* allowed;
+  int64_t allowed_stride; /* words, >= ceil(vocab_size / 32) */
+  const uint8_t* mask;
+} PaceLogits;
+
+/* For every row, over its places that are not excluded, with m the largest
+ * logit, t the temperature and S = sum_j exp((z_j - m) / t):
+ *   logprob = (z_y - m) / t - ln S      (-inf where the target y is excluded)
+ *   lse     = m / t + ln S
+ *   entropy = ln S - (1 / S) sum_j exp((z_j - m) / t) (z_j - m) / t
+ *   stats   = {m, ln S}, which the backward takes (m and ln S apart keep the
+ *             probabilities exact however large the logits are)
+ *   top_ids, top_logprob [top_k]: the places of the largest logits, equal logits
+ *             lowest place first, and their log-probs; -1 and -inf where the row
+ *             has fewer places.
+ * A row without places has logprob and lse -inf, entropy 0, stats {-inf, 0} and no
+ * alternatives.  A row that holds NaN or +inf in a place that is not excluded has
+ * NaN in every float32 output (top_ids -1) and PACE_ERR_NAN_INPUT is reported; a
+ * target outside the vocabulary has logprob NaN and PACE_ERR_INVALID_ARG.
+ *   targets     device int32 [n_rows], or NULL together with logprob.
+ *   logprob, entropy, lse   device float32 [n_rows]; stats device float32
+ *               [n_rows][2]; any may be NULL.
+ *   top_k       0..64; top_ids device int32, top_logprob device float32
+ *               [n_rows][top_k] (NULL when top_k is 0).
+ * One launch reads every logit once (a few hundred bytes an alternative again),
+ * without workspace; sums are in float32, in a fixed order for given sizes. */
+PACE_API pace_status pace_logits_logprob(const PaceLogits* logits, const int32_t* targets,
+                                         float temperature, int32_t top_k, float* logprob,
+                                         float* entropy, float* lse, float* stats,
+                                         int32_t* top_ids, float* top_logprob,
+                                         int32_t* status_dev, void* stream);
+
+/* Gradient with respect to the logits of sum_r dlp_r logprob_r + dentropy_r entropy_r:
+ *   grad_j = (dlp / t) (1[j = y] - p_j) - (dentropy / t) p_j (ln p_j + entropy)
+ * with ln p_j = (z_j - m) / t - ln S; 0 at excluded places, in rows outside the
+ * mask and in rows without places.
+ *   stats, entropy   as the forward wrote them for these logits (entropy may be
+ *               NULL when dentropy is).
+ *   dlp         device float32 [n_rows]; dentropy the same or NULL (0).
+ *   grad        device, of the logits' dtype, row r at grad + r * grad_stride; it
+ *               may be the logits' own buffer (same pointer and stride), and must
+ *               not overlap them otherwise.
+ * A target outside the vocabulary reports PACE_ERR_INVALID_ARG. */
+PACE_API pace_status pace_logits_logprob_backward(const PaceLogits* logits,
+                                                  const int32_t* targets, float temperature,
+                                                  const float* stats, const float* entropy,
+                                                  const float* dlp, const float* dentropy,
+                                                  void* grad, int64_t grad_stride,
+                                                  int32_t* status_dev, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Profiling                                                                 */
 /* ------------------------------------------------------------------------ */
 

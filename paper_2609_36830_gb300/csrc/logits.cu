@@ -1,0 +1,763 @@
+// Log-probabilities of given tokens, entropy and top alternatives from logits in
+// memory, and the gradient of the first two with respect to the logits.
+//
+// Forward, with m the largest logit of a row's places, t the temperature:
+//   S = sum e^((z - m) / t),   T = sum e^((z - m) / t) (z - m)
+//   lp = (z_y - m) / t - ln S,   H = ln S - T / (t S)
+// Both terms of H are >= 0, so a peaked row loses nothing to cancellation.  One pass: a
+// lane keeps (m, S, T) over its logits and rescales them when its maximum grows.
+//
+// Alternatives without a second pass: the row is cut into chunks of 32 vectors of 16
+// bytes (one load of a warp), whose maxima the pass has at hand.  A logit among the k
+// first (by value, equal ones lowest place first) lies in one of the k first chunks
+// (by maximum, equal ones lowest first): every chunk before its own holds a logit
+// before it.  The same holds for the 16-byte vectors of those chunks, and for the
+// logits of the k first vectors.  So k chunks are read again, then k vectors: 512 k
+// bytes of a row's 300 KB, and nothing depends on how many logits are equal.
+#include <float.h>
+#include <math.h>
+
+#include <type_traits>
+
+#include "pace_internal.cuh"
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+namespace pace {
+namespace {
+
+constexpr int kTopMax = 64;
+constexpr int kMaxWarps = 8;
+constexpr int kMaxCluster = 8;
+constexpr int kUnroll = 4;             // chunks a warp has in flight
+constexpr uint32_t kNoPlace = 0x007FFFFFu;  // order_key(-inf)
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ------------------------------------------------------------- logit types
+
+template <typename T>
+struct Logit;
+template <>
+struct Logit<float> {
+  static constexpr int kPer = 4;
+  static constexpr uint32_t kNegInf = 0xFF800000u;
+  static __device__ void unpack(const uint4& v, float (&f)[4]) {
+    f[0] = __uint_as_float(v.x);
+    f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z);
+    f[3] = __uint_as_float(v.w);
+  }
+  static __device__ uint4 pack(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                      __float_as_uint(f[3]));
+  }
+  static __device__ float value(float x) { return x; }
+  static __device__ float from(float x) { return x; }
+};
+template <>
+struct Logit<__nv_bfloat16> {
+  static constexpr int kPer = 8;
+  static constexpr uint32_t kNegInf = 0xFF80FF80u;
+  static __device__ void unpack(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ uint4 pack(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
+  static __device__ __nv_bfloat16 from(float x) { return __float2bfloat16_rn(x); }
+};
+template <>
+struct Logit<__half> {
+  static constexpr int kPer = 8;
+  static constexpr uint32_t kNegInf = 0xFC00FC00u;
+  static __device__ void unpack(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      f[2 * i] = p.x;
+      f[2 * i + 1] = p.y;
+    }
+  }
+  static __device__ uint4 pack(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ float value(__half x) { return __half2float(x); }
+  static __device__ __half from(float x) { return __float2half_rn(x); }
+};
+
+// ------------------------------------------------------------- small pieces
+
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+__device__ __forceinline__ float warp_max_nan(float v) {
+  float r;
+  asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) v += __shfl_xor_sync(0xffffffffu, v, x);
+  return v;
+}
+
+// Unsigned integers in the order of the floats; -0 and +0 are one.
+__device__ __forceinline__ uint32_t order_key(float f) {
+  const uint32_t b = __float_as_uint(f + 0.0f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+}
+
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t a) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+  return v;
+}
+
+// The softmax sums of some of a row's logits (above); S = 0 without any.
+struct Sums {
+  float m, s, t;
+};
+
+// What `a` becomes when its maximum is raised to `m` (finite).
+__device__ __forceinline__ Sums raised(const Sums& a, float m, float k) {
+  const float d = fmaxf(a.m - m, -FLT_MAX);  // (a.m may be -inf)
+  const float f = ex2_approx(d * k);
+  // f = 0: nothing is left, and d s may be infinite
+  return {m, a.s * f, f > 0.0f ? f * fmaf(d, a.s, a.t) : 0.0f};
+}
+
+// One row: where it starts, and which of its places count.
+template <typename T>
+struct Row {
+  static constexpr int kPer = Logit<T>::kPer;
+  const T* z;
+  int shift;  // places before the row in its first 16-byte vector
+  int V;
+  const uint32_t* allowed;  // or null
+
+  __device__ Row(const PaceLogits& p, int64_t r)
+      : z(static_cast<const T*>(p.logits) + r * p.row_stride), V(p.vocab_size),
+        allowed(p.allowed ? p.allowed + r * p.allowed_stride : nullptr) {
+    shift = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
+  }
+  __device__ int vectors() const { return (shift + V + kPer - 1) / kPer; }
+  __device__ bool inside(int v) const {  // whole
+    return v * kPer >= shift && (v + 1) * kPer <= shift + V;
+  }
+  // Vector v's 16 bytes, -inf at the places outside the row.
+  __device__ uint4 load(int v) const {
+    const int j0 = v * kPer - shift;
+    if (inside(v)) return *reinterpret_cast<const uint4*>(z + j0);
+    uint4 raw = make_uint4(Logit<T>::kNegInf, Logit<T>::kNegInf, Logit<T>::kNegInf,
+                           Logit<T>::kNegInf);
+    T* e = reinterpret_cast<T*>(&raw);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (j0 + i >= 0 && j0 + i < V) e[i] = z[j0 + i];
+    return raw;
+  }
+  // Bits of the allowed places of vector v (others of its bits are arbitrary).
+  __device__ uint32_t bits(int v) const {
+    const int j0 = v * kPer - shift, w = j0 >> 5, sh = j0 & 31;
+    const int last = (V - 1) >> 5;
+    const uint32_t lo = w >= 0 && w <= last ? allowed[w] : 0u;
+    const uint32_t hi = sh > 32 - kPer && w + 1 <= last ? allowed[w + 1] : 0u;
+    return __funnelshift_r(lo, hi, sh);
+  }
+  __device__ bool allows(int j) const {
+    return !allowed || (allowed[j >> 5] >> (j & 31) & 1u);
+  }
+};
+
+// ------------------------------------------------------------- the kernels
+
+struct ForwardArgs {
+  PaceLogits lg;
+  const int32_t* targets;
+  float k;      // log2(e) / t
+  float inv_t;
+  int top;
+  int cluster;  // CTAs a row
+  float *logprob, *entropy, *lse, *stats, *top_logprob;
+  int32_t* top_ids;
+  int32_t* status;
+};
+
+// Positions of the kk first of n keys (by key, equal ones lowest position first),
+// ascending, and a key that none of them is below.  One warp calls it; kk <= n.
+__device__ uint32_t select_first(const uint32_t* keys, int n, int kk, int lane, int* out) {
+  const unsigned full = 0xffffffffu;
+  uint32_t lo = 0xffffffffu, hi = 0u;
+  for (int i = lane; i < n; i += 32) {
+    lo = min(lo, keys[i]);
+    hi = max(hi, keys[i]);
+  }
+  lo = __reduce_min_sync(full, lo);
+  hi = __reduce_max_sync(full, hi);
+  uint32_t t = lo;
+  if (kk < n && lo != hi) {
+    // the largest t that at least kk keys reach, bit by bit below their common prefix
+    const int b = 31 - __clz(lo ^ hi);
+    t = hi & ~((2u << b) - 1u);
+    for (int bit = b; bit >= 0; --bit) {
+      const uint32_t u = t | (1u << bit);
+      int c = 0;
+      for (int i = lane; i < n; i += 32) c += keys[i] >= u;
+      c = __reduce_add_sync(full, c);
+      if (c >= kk) t = u;
+      if (c == kk) break;
+    }
+  }
+  int above = 0;
+  for (int i = lane; i < n; i += 32) above += keys[i] > t;
+  int ties = kk - __reduce_add_sync(full, above);
+  int at = 0;
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    const uint32_t key = i0 + lane < n ? keys[i0 + lane] : 0u;
+    const bool in = i0 + lane < n;
+    const uint32_t eq = __ballot_sync(full, in && key == t);
+    const uint32_t below = (1u << lane) - 1u;
+    const bool take = in && (key > t || (key == t && __popc(eq & below) < ties));
+    const uint32_t got = __ballot_sync(full, take);
+    if (take) out[at + __popc(got & below)] = i0 + lane;
+    at += __popc(got);
+    ties -= min(ties, __popc(eq));
+    if (at == kk) break;
+  }
+  return t;
+}
+
+// n candidate keys (value key << 32 | ~place, distinct) into list[0 .. k), largest
+// first; list is zero where there are fewer.  The whole block calls it.
+__device__ void rank_keys(const unsigned long long* cand, int n, int k,
+                          unsigned long long* list) {
+  for (int i = threadIdx.x; i < k; i += blockDim.x) list[i] = 0ull;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const unsigned long long key = cand[i];
+    if (key == 0ull) continue;
+    int before = 0;
+    for (int j = 0; j < n; ++j) before += cand[j] > key;
+    if (before < k) list[before] = key;
+  }
+  __syncthreads();
+}
+
+struct TopShared {
+  int chunk[kTopMax];
+  int vec[kTopMax];
+  uint32_t vkey[kTopMax * 32];
+  unsigned long long cand[kTopMax * 8];
+  unsigned long long list[kTopMax];
+  uint32_t least;
+  int n_cand;
+};
+struct NoShared {};
+
+template <typename T, bool kAllowed, bool kTop>
+__global__ void __launch_bounds__(kMaxWarps * 32)
+    logits_logprob_kernel(const ForwardArgs p) {
+  constexpr int kPer = Logit<T>::kPer;
+  extern __shared__ uint32_t ckey[];  // kTop: the maxima of this CTA's chunks, as keys
+  __shared__ Sums s_warp[kMaxWarps];
+  __shared__ Sums s_cta, s_row;
+  __shared__ typename std::conditional<kTop, TopShared, NoShared>::type s_top;
+  const int C = p.cluster;
+  const int64_t r = blockIdx.x / C;
+  const int rank = static_cast<int>(blockIdx.x % C);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  if (p.lg.mask && p.lg.mask[r] == 0) {  // the same for the row's CTAs
+    if (rank == 0) {
+      if (threadIdx.x == 0) {
+        if (p.logprob) p.logprob[r] = 0.0f;
+        if (p.entropy) p.entropy[r] = 0.0f;
+        if (p.lse) p.lse[r] = 0.0f;
+        if (p.stats) reinterpret_cast<float2*>(p.stats)[r] = make_float2(0.0f, 0.0f);
+      }
+      for (int i = threadIdx.x; i < p.top; i += blockDim.x) {
+        p.top_ids[r * p.top + i] = -1;
+        p.top_logprob[r * p.top + i] = -INFINITY;
+      }
+    }
+    return;
+  }
+  const Row<T> row(p.lg, r);
+  // the target's logit is on its way while the row is read
+  int32_t y = 0;
+  float zy = 0.0f;
+  bool y_in = false;
+  if (rank == 0 && threadIdx.x == 0 && p.logprob) {
+    y = p.targets[r];
+    y_in = y >= 0 && y < row.V;
+    if (y_in) zy = row.allows(y) ? Logit<T>::value(row.z[y]) : -INFINITY;
+  }
+  const int n_vec = row.vectors(), n_chunks = (n_vec + 31) / 32;
+  const int c0 = static_cast<int>(static_cast<int64_t>(n_chunks) * rank / C);
+  const int c1 = static_cast<int>(static_cast<int64_t>(n_chunks) * (rank + 1) / C);
+
+  Sums a{-INFINITY, 0.0f, 0.0f};
+  for (int c = c0 + warp * kUnroll; c < c1; c += warps * kUnroll) {
+    uint4 raw[kUnroll];
+    uint32_t bits[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int v = (c + u) * 32 + lane;
+      const bool on = c + u < c1 && v < n_vec;
+      raw[u] = make_uint4(Logit<T>::kNegInf, Logit<T>::kNegInf, Logit<T>::kNegInf,
+                          Logit<T>::kNegInf);
+      if (on) raw[u] = row.load(v);
+      if (kAllowed) bits[u] = on ? row.bits(v) : 0u;
+    }
+    float f[kUnroll][kPer];
+    float m = a.m;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      Logit<T>::unpack(raw[u], f[u]);
+      if (kAllowed) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) f[u][i] = bits[u] >> i & 1u ? f[u][i] : -INFINITY;
+      }
+      float vm = f[u][0];
+#pragma unroll
+      for (int i = 1; i < kPer; ++i) vm = max_nan(vm, f[u][i]);
+      m = max_nan(m, vm);
+      if (kTop) {
+        const float cm = warp_max_nan(vm);
+        if (lane == 0 && c + u < c1) ckey[c + u - c0] = order_key(cm);
+      }
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+    a = raised(a, ref, p.k);
+    a.m = m;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const float d = fmaxf(f[u][i] - ref, -FLT_MAX);
+        const float e = ex2_approx(d * p.k);
+        a.s += e;
+        a.t = fmaf(e, d, a.t);
+      }
+    }
+  }
+
+  // lanes, warps and CTAs: sums against the common maximum, added in a fixed order
+  auto merge = [&](const Sums& x) {
+    const float m = warp_max_nan(x.m);
+    Sums y2 = raised(x, m == -INFINITY ? 0.0f : m, p.k);
+    return Sums{m, warp_sum(y2.s), warp_sum(y2.t)};
+  };
+  const Sums none{-INFINITY, 0.0f, 0.0f};
+  const Sums w = merge(a);
+  if (lane == 0) s_warp[warp] = w;
+  __syncthreads();
+  if (warp == 0) {
+    const Sums c = merge(lane < warps ? s_warp[lane] : none);
+    if (lane == 0) {
+      s_cta = c;
+      if (C == 1) s_row = c;
+    }
+  }
+
+  if constexpr (kTop) {
+    const int n_c = c1 - c0;
+    const int k1 = min(p.top, n_c);
+    if (warp == 0) select_first(ckey, n_c, k1, lane, s_top.chunk);
+    if (threadIdx.x == 0) s_top.n_cand = 0;
+    __syncthreads();
+    for (int i = warp; i < k1; i += warps) {
+      const int v = (c0 + s_top.chunk[i]) * 32 + lane;
+      float vm = -INFINITY;
+      if (v < n_vec) {
+        float f[kPer];
+        Logit<T>::unpack(row.load(v), f);
+        const uint32_t b = kAllowed ? row.bits(v) : 0xffffffffu;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) vm = fmaxf(vm, b >> e & 1u ? f[e] : -INFINITY);
+      }
+      s_top.vkey[i * 32 + lane] = order_key(vm);
+    }
+    __syncthreads();
+    const int k2 = min(p.top, k1 * 32);
+    if (warp == 0) {
+      const uint32_t least = select_first(s_top.vkey, k1 * 32, k2, lane, s_top.vec);
+      // with fewer vectors than alternatives, every place of theirs is a candidate
+      if (lane == 0) s_top.least = k2 == p.top ? max(least, kNoPlace + 1u) : kNoPlace + 1u;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < k2 * kPer; i += blockDim.x) {
+      const int at = s_top.vec[i / kPer];
+      const int v = (c0 + s_top.chunk[at >> 5]) * 32 + (at & 31);
+      const int j = v * kPer - row.shift + i % kPer;
+      if (j < 0 || j >= row.V || !row.allows(j)) continue;
+      const uint32_t key = order_key(Logit<T>::value(row.z[j]));
+      if (key >= s_top.least)
+        s_top.cand[atomicAdd(&s_top.n_cand, 1)] =
+            static_cast<unsigned long long>(key) << 32 | (0xffffffffu - static_cast<uint32_t>(j));
+    }
+    __syncthreads();
+    rank_keys(s_top.cand, s_top.n_cand, p.top, s_top.list);
+  } else {
+    __syncthreads();
+  }
+
+  if (C > 1) {
+    cluster_sync();  // every CTA's sums and list are in its shared memory
+    if (rank == 0) {
+      if (warp == 0) {
+        Sums x = none;
+        if (lane < C) {
+          const uint32_t at = cluster_addr(&s_cta, lane);
+          x.m = __uint_as_float(ld_cluster_u32(at));
+          x.s = __uint_as_float(ld_cluster_u32(at + 4));
+          x.t = __uint_as_float(ld_cluster_u32(at + 8));
+        }
+        const Sums c = merge(x);
+        if (lane == 0) s_row = c;
+      }
+      if constexpr (kTop) {
+        for (int i = threadIdx.x; i < C * p.top; i += blockDim.x)
+          s_top.cand[i] = ld_cluster_u64(cluster_addr(&s_top.list[i % p.top], i / p.top));
+      }
+    }
+    cluster_sync();  // read: the other CTAs may leave
+    if (rank != 0) return;
+    if constexpr (kTop) rank_keys(s_top.cand, C * p.top, p.top, s_top.list);
+  }
+
+  const Sums all = s_row;
+  const bool empty = all.m == -INFINITY;
+  const bool bad = !(all.m < INFINITY);  // NaN or +inf among the places
+  const float nan = __int_as_float(0x7fc00000);
+  const float log_s = empty ? 0.0f : logf(all.s);
+  if (threadIdx.x == 0) {
+    if (bad) report(p.status, PACE_ERR_NAN_INPUT);
+    if (p.logprob) {
+      float lp = y_in ? (empty || zy == -INFINITY ? -INFINITY : (zy - all.m) * p.inv_t - log_s)
+                      : nan;
+      if (!y_in) report(p.status, PACE_ERR_INVALID_ARG);
+      p.logprob[r] = bad ? nan : lp;
+    }
+    if (p.lse) p.lse[r] = bad ? nan : (empty ? -INFINITY : fmaf(all.m, p.inv_t, log_s));
+    if (p.entropy)
+      p.entropy[r] = bad ? nan : (empty ? 0.0f : log_s - all.t / all.s * p.inv_t);
+    if (p.stats)
+      reinterpret_cast<float2*>(p.stats)[r] =
+          bad ? make_float2(nan, nan) : make_float2(all.m, log_s);
+  }
+  if constexpr (kTop) {
+    for (int i = threadIdx.x; i < p.top; i += blockDim.x) {
+      const unsigned long long key = s_top.list[i];
+      const bool there = key != 0ull && !bad;
+      const float z = key_value(static_cast<uint32_t>(key >> 32));
+      p.top_ids[r * p.top + i] =
+          there ? static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(key)) : -1;
+      p.top_logprob[r * p.top + i] =
+          there ? (z - all.m) * p.inv_t - log_s : (bad ? nan : -INFINITY);
+    }
+  }
+}
+
+struct BackwardArgs {
+  PaceLogits lg;
+  const int32_t* targets;
+  float k, inv_t;
+  const float *stats, *entropy, *dlp, *dent;
+  void* grad;
+  int64_t grad_stride;
+  int pieces;  // blocks a row
+  int32_t* status;
+};
+
+constexpr int kBwThreads = 256;
+constexpr int kBwVecs = 4;  // 16-byte vectors a thread
+
+// A block per piece of a row.  Vectors are those of the gradient's row; where the
+// logits' row starts elsewhere in its 16 bytes, they are read place by place.
+template <typename T, bool kAllowed, bool kEntropy>
+__global__ void __launch_bounds__(kBwThreads) logits_backward_kernel(const BackwardArgs p) {
+  constexpr int kPer = Logit<T>::kPer;
+  const int64_t r = blockIdx.x / p.pieces;
+  const int piece = static_cast<int>(blockIdx.x % p.pieces);
+  const Row<T> row(p.lg, r);
+  T* g = static_cast<T*>(p.grad) + r * p.grad_stride;
+  const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(g) & 15) / sizeof(T));
+  const bool same = shift == row.shift;
+  const int n_vec = (shift + row.V + kPer - 1) / kPer;
+  const int v0 = piece * (kBwThreads * kBwVecs) + threadIdx.x;
+  const bool in = !p.lg.mask || p.lg.mask[r] != 0;
+  const float2 st = reinterpret_cast<const float2*>(p.stats)[r];
+  const bool live = in && st.x != -INFINITY;
+  const float gl = live ? p.dlp[r] * p.inv_t : 0.0f;
+  float ge = 0.0f, h = 0.0f;
+  if (kEntropy && live) {
+    ge = p.dent[r] * p.inv_t;
+    h = p.entropy[r];
+  }
+  int32_t y = -1;
+  if (live) {
+    y = p.targets[r];
+    if (y < 0 || y >= row.V) {
+      if (piece == 0 && threadIdx.x == 0) report(p.status, PACE_ERR_INVALID_ARG);
+      y = -1;
+    }
+  }
+  const float l2s = st.y * kLog2e;
+  uint4 raw[kBwVecs];
+  uint32_t bits[kBwVecs];
+#pragma unroll
+  for (int u = 0; u < kBwVecs; ++u) {
+    const int v = v0 + u * kBwThreads;
+    raw[u] = make_uint4(0, 0, 0, 0);
+    bits[u] = 0xffffffffu;
+    if (live && v < n_vec) {
+      const int j0 = v * kPer - shift;
+      if (same) {
+        raw[u] = row.load(v);
+        if (kAllowed) bits[u] = row.bits(v);
+      } else {
+        T* e = reinterpret_cast<T*>(&raw[u]);
+        uint32_t b = 0u;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (j0 + i >= 0 && j0 + i < row.V) {
+            e[i] = row.z[j0 + i];
+            if (kAllowed) b |= static_cast<uint32_t>(row.allows(j0 + i)) << i;
+          }
+        if (kAllowed) bits[u] = b;
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kBwVecs; ++u) {
+    const int v = v0 + u * kBwThreads;
+    if (v >= n_vec) break;
+    const int j0 = v * kPer - shift;
+    float f[kPer];
+    Logit<T>::unpack(raw[u], f);
+    if (live) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const float z = !kAllowed || (bits[u] >> i & 1u) ? f[i] : -INFINITY;
+        const float lp2 = fmaxf(fmaf(z - st.x, p.k, -l2s), -1e30f);  // log2 p, finite
+        const float pr = ex2_approx(lp2);
+        float x = gl;
+        if (kEntropy) x = fmaf(ge, fmaf(lp2, 0.69314718f, h), x);
+        x = -pr * x;
+        f[i] = j0 + i == y && z != -INFINITY ? x + gl : x;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) f[i] = 0.0f;
+    }
+    if (j0 >= 0 && j0 + kPer <= row.V) {
+      *reinterpret_cast<uint4*>(g + j0) = Logit<T>::pack(f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (j0 + i >= 0 && j0 + i < row.V) g[j0 + i] = Logit<T>::from(f[i]);
+    }
+  }
+}
+
+// ------------------------------------------------------------- host side
+
+size_t element_bytes(int32_t dtype) { return dtype == PACE_F32 ? 4 : 2; }
+
+pace_status check_logits(const PaceLogits* l) {
+  if (!l || l->n_rows < 0) return PACE_ERR_INVALID_ARG;
+  if (l->dtype != PACE_F32 && l->dtype != PACE_BF16 && l->dtype != PACE_F16)
+    return PACE_ERR_INVALID_ARG;
+  if (l->vocab_size < 1 || l->vocab_size > (1 << 24) || l->n_rows > (int64_t{1} << 28))
+    return PACE_ERR_UNSUPPORTED_SHAPE;
+  if (l->row_stride < l->vocab_size) return PACE_ERR_INVALID_ARG;
+  if (l->allowed && l->allowed_stride < (l->vocab_size + 31) / 32) return PACE_ERR_INVALID_ARG;
+  if (l->n_rows > 0 && !l->logits) return PACE_ERR_INVALID_ARG;
+  if (!aligned(l->logits, element_bytes(l->dtype)) || !aligned(l->allowed, 4))
+    return PACE_ERR_UNSUPPORTED_SHAPE;
+  return PACE_OK;
+}
+
+pace_status check_temperature(float t) {
+  // (a subnormal temperature has no finite reciprocal)
+  return t > 0.0f && isfinite(t) && isfinite(kLog2e / t) ? PACE_OK : PACE_ERR_INVALID_ARG;
+}
+
+// CTAs (a cluster) and warps for each row.  A wave wants some eight warps on every
+// scheduler; below that the row is split, but not into slices of less than a warp's
+// four chunks.  A CTA's chunk maxima take 4 bytes each of shared memory, so rows of
+// more than 8,192 chunks are split too.
+struct RowSplit {
+  int cluster, warps;
+};
+RowSplit split_row(int64_t n_rows, int n_chunks) {
+  RowSplit s{1, 1};
+  while (s.warps < kMaxWarps && s.warps * kUnroll < n_chunks) s.warps *= 2;
+  const int64_t want = static_cast<int64_t>(sm_count()) * 4;
+  while (s.cluster < kMaxCluster && n_rows * s.cluster < want &&
+         2 * s.cluster * s.warps * kUnroll <= n_chunks)
+    s.cluster *= 2;
+  while (s.cluster < kMaxCluster && n_chunks > 8192 * s.cluster) s.cluster *= 2;
+  return s;
+}
+
+template <typename T, bool kAllowed, bool kTop>
+pace_status launch_forward(ForwardArgs a, cudaStream_t st) {
+  constexpr int kPer = Logit<T>::kPer;
+  // a row may begin anywhere in its first vector
+  const int n_vec = (kPer - 1 + a.lg.vocab_size + kPer - 1) / kPer;
+  const int n_chunks = (n_vec + 31) / 32;
+  const RowSplit s = split_row(a.lg.n_rows, n_chunks);
+  a.cluster = s.cluster;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(a.lg.n_rows * s.cluster), 1, 1);
+  cfg.blockDim = dim3(static_cast<unsigned>(s.warps) * 32, 1, 1);
+  cfg.dynamicSmemBytes = kTop ? static_cast<size_t>(n_chunks / s.cluster + 1) * 4 : 0;
+  cfg.stream = st;
+  if (cfg.dynamicSmemBytes > 32768)  // (float32 rows of more than 8.4M places)
+    PACE_TRY_CUDA(cudaFuncSetAttribute(logits_logprob_kernel<T, kAllowed, kTop>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(cfg.dynamicSmemBytes)));
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = static_cast<unsigned>(s.cluster);
+  attr.val.clusterDim.y = 1;
+  attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = s.cluster > 1 ? 1 : 0;
+  if (cudaLaunchKernelEx(&cfg, logits_logprob_kernel<T, kAllowed, kTop>, a) != cudaSuccess) {
+    cudaGetLastError();
+    return PACE_ERR_CUDA;
+  }
+  return last_launch_status();
+}
+
+template <typename T>
+pace_status launch_forward_of(const ForwardArgs& a, cudaStream_t st) {
+  if (a.lg.allowed)
+    return a.top ? launch_forward<T, true, true>(a, st) : launch_forward<T, true, false>(a, st);
+  return a.top ? launch_forward<T, false, true>(a, st) : launch_forward<T, false, false>(a, st);
+}
+
+template <typename T>
+pace_status launch_backward_of(BackwardArgs a, cudaStream_t st) {
+  constexpr int kPer = Logit<T>::kPer;
+  const int n_vec = (kPer - 1 + a.lg.vocab_size + kPer - 1) / kPer;
+  a.pieces = (n_vec + kBwThreads * kBwVecs - 1) / (kBwThreads * kBwVecs);
+  const int64_t blocks = a.lg.n_rows * a.pieces;
+  if (blocks > INT32_MAX) return PACE_ERR_UNSUPPORTED_SHAPE;
+  const unsigned grid = static_cast<unsigned>(blocks);
+  if (a.lg.allowed) {
+    if (a.dent) logits_backward_kernel<T, true, true><<<grid, kBwThreads, 0, st>>>(a);
+    else logits_backward_kernel<T, true, false><<<grid, kBwThreads, 0, st>>>(a);
+  } else {
+    if (a.dent) logits_backward_kernel<T, false, true><<<grid, kBwThreads, 0, st>>>(a);
+    else logits_backward_kernel<T, false, false><<<grid, kBwThreads, 0, st>>>(a);
+  }
+  return last_launch_status();
+}
+
+}  // namespace
+}  // namespace pace
+
+using namespace pace;
+
+extern "C" pace_status pace_logits_logprob(const PaceLogits* logits, const int32_t* targets,
+                                           float temperature, int32_t top_k, float* logprob,
+                                           float* entropy, float* lse, float* stats,
+                                           int32_t* top_ids, float* top_logprob,
+                                           int32_t* status_dev, void* stream) {
+  PACE_TRY(check_logits(logits));
+  PACE_TRY(check_temperature(temperature));
+  if (top_k < 0) return PACE_ERR_INVALID_ARG;
+  if (top_k > kTopMax) return PACE_ERR_UNSUPPORTED_SHAPE;
+  if (logits->n_rows > 0) {
+    if (logprob && !targets) return PACE_ERR_INVALID_ARG;
+    if (top_k > 0 && (!top_ids || !top_logprob)) return PACE_ERR_INVALID_ARG;
+  }
+  if (!aligned(stats, 8)) return PACE_ERR_UNSUPPORTED_SHAPE;
+  if (logits->n_rows == 0) return PACE_OK;
+  ForwardArgs a;
+  a.lg = *logits;
+  a.targets = targets;
+  a.k = kLog2e / temperature;
+  a.inv_t = 1.0f / temperature;
+  a.top = top_k;
+  a.cluster = 1;
+  a.logprob = logprob;
+  a.entropy = entropy;
+  a.lse = lse;
+  a.stats = stats;
+  a.top_ids = top_ids;
+  a.top_logprob = top_logprob;
+  a.status = status_dev;
+  cudaStream_t st = as_stream(stream);
+  switch (logits->dtype) {
+    case PACE_F32: return launch_forward_of<float>(a, st);
+    case PACE_BF16: return launch_forward_of<__nv_bfloat16>(a, st);
+    default: return launch_forward_of<__half>(a, st);
+  }
+}
+
+extern "C" pace_status pace_logits_logprob_backward(const PaceLogits* logits,
+                                                    const int32_t* targets, float temperature,
+                                                    const float* stats, const float* entropy,
+                                                    const float* dlp, const float* dentropy,
+                                                    void* grad, int64_t grad_stride,
+                                                    int32_t* status_dev, void* stream) {
+  PACE_TRY(check_logits(logits));
+  PACE_TRY(check_temperature(temperature));
+  if (grad_stride < logits->vocab_size) return PACE_ERR_INVALID_ARG;
+  if (logits->n_rows > 0 && (!targets || !stats || !dlp || !grad || (dentropy && !entropy)))
+    return PACE_ERR_INVALID_ARG;
+  if (!aligned(grad, element_bytes(logits->dtype)) || !aligned(stats, 8))
+    return PACE_ERR_UNSUPPORTED_SHAPE;
+  if (logits->n_rows == 0) return PACE_OK;
+  BackwardArgs a;
+  a.lg = *logits;
+  a.targets = targets;
+  a.k = kLog2e / temperature;
+  a.inv_t = 1.0f / temperature;
+  a.stats = stats;
+  a.entropy = entropy;
+  a.dlp = dlp;
+  a.dent = dentropy;
+  a.grad = grad;
+  a.grad_stride = grad_stride;
+  a.pieces = 1;
+  a.status = status_dev;
+  cudaStream_t st = as_stream(stream);
+  switch (logits->dtype) {
+    case PACE_F32: return launch_backward_of<float>(a, st);
+    case PACE_BF16: return launch_backward_of<__nv_bfloat16>(a, st);
+    default: return launch_backward_of<__half>(a, st);
+  }
+}

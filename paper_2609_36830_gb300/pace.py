@@ -63,6 +63,11 @@ class PaceLossArgs(ctypes.Structure):
                 ("partial", _P)]
 
 
+class PaceLogits(ctypes.Structure):
+    _fields_ = [("logits", _P), ("dtype", _I32), ("vocab_size", _I32), ("n_rows", _I64),
+                ("row_stride", _I64), ("allowed", _P), ("allowed_stride", _I64), ("mask", _P)]
+
+
 # every symbol include/pace.h declares, with its C signature
 SIGNATURES = {
     "pace_status_string": ([_I32], ctypes.c_char_p),
@@ -102,6 +107,8 @@ SIGNATURES = {
     "pace_token_logprob_backward": ([_P, _P, _P, _P, _I32, _I32, _F32, _P, _P, _P, _P, _P, _SZ,
                                      _P, _P], _I32),
     "pace_token_logprob_backward_workspace_size": ([_I64, _I64, _I32, _I32], _SZ),
+    "pace_logits_logprob": ([_P, _P, _F32, _I32, _P, _P, _P, _P, _P, _P, _P, _P], _I32),
+    "pace_logits_logprob_backward": ([_P, _P, _F32, _P, _P, _P, _P, _P, _I64, _P, _P], _I32),
     "pace_set_profile_events": ([_I32, _P, _P], _I32),
     "pace_set_lmhead_splits": ([_I32], _I32),
     "pace_set_score_fused_min_traj": ([_I64], _I32),
@@ -180,6 +187,31 @@ def _refuse(t, dtype, n, name):
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
     raise ValueError(f"{name}: needs at least {n} elements, has {t.numel()}")
+
+
+# pace_dtype
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _rows_arg(t, dtypes, shape, name: str):
+    """(device pointer, row stride) of a 2-D tensor of one of `dtypes` whose rows are
+    contiguous, of shape `shape` (None: any) on the current CUDA device."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if not t.is_cuda or t.get_device() != _current_device():
+        raise ValueError(f"{name}: expected a tensor on the current CUDA device")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: expected {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: expected shape {shape or '[rows, columns]'}, got "
+                         f"{tuple(t.shape)}")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: expected contiguous rows")
+    stride = t.stride(0) if rows > 1 else cols
+    if stride < cols:
+        raise ValueError(f"{name}: rows overlap (stride {stride}, {cols} columns)")
+    return t.data_ptr(), stride
 
 
 _U8, _I32T, _I64T = torch.uint8, torch.int32, torch.int64
@@ -618,3 +650,76 @@ def token_logprob_backward(batch: PaceBatch, hidden, w_vocab, targets, lse, dlp,
                                            _arg(status, _I32T, 1, "status"), _stream(stream))
     _check(st, "pace_token_logprob_backward")
     return grad_hidden, grad_w
+
+
+# ---------------------------------------------------------------- logits in memory
+
+def make_logits(logits, allowed=None, mask=None):
+    """PaceLogits of a float32, bf16 or fp16 tensor [n_rows, V] with contiguous rows (any
+    row stride).  allowed: int32 [n_rows, >= ceil(V / 32)], a bit per place; mask: uint8
+    [n_rows], 0 for rows that are left out."""
+    ptr, stride = _rows_arg(logits, tuple(_DTYPES), None, "logits")
+    n, V = logits.shape
+    a_ptr, a_stride = None, 0
+    if allowed is not None:
+        a_ptr, a_stride = _rows_arg(allowed, (_I32T,), None, "allowed")
+        if allowed.shape[0] != n or allowed.shape[1] < (V + 31) // 32:
+            raise ValueError(f"allowed: expected [{n}, {(V + 31) // 32}] words, got "
+                             f"{tuple(allowed.shape)}")
+        if n <= 1:
+            a_stride = allowed.shape[1]
+    lg = PaceLogits(ptr, _DTYPES[logits.dtype], V, n, stride, a_ptr, a_stride,
+                    _arg(mask, _U8, n, "mask"))
+    lg._keep = (logits, allowed, mask)  # keep the tensors alive with the struct
+    return lg
+
+
+def logits_logprob_outputs(n_rows, top_k=0, device="cuda"):
+    """The output buffers of logits_logprob, for a program that keeps them."""
+    f = dict(dtype=torch.float32, device=device)
+    out = {k: torch.empty(n_rows, **f) for k in ("logprob", "entropy", "lse")}
+    out["stats"] = torch.empty((n_rows, 2), **f)
+    if top_k:
+        out["top_ids"] = torch.empty((n_rows, top_k), dtype=torch.int32, device=device)
+        out["top_logprob"] = torch.empty((n_rows, top_k), **f)
+    return out
+
+
+def logits_logprob(lg: PaceLogits, targets=None, temperature=1.0, top_k=0, out=None,
+                   status=None, stream=None):
+    """pace_logits_logprob.  Returns dict logprob (with targets), entropy, lse [n_rows],
+    stats [n_rows, 2] and, with top_k > 0, top_ids int32 and top_logprob [n_rows, top_k].
+    Of `out`, what it holds is written."""
+    n, k = lg.n_rows, int(top_k)
+    if out is None:
+        out = logits_logprob_outputs(n, k, lg._keep[0].device)
+        if targets is None:
+            del out["logprob"]
+    st = lib().pace_logits_logprob(
+        ctypes.byref(lg), _arg(targets, _I32T, n, "targets"), float(temperature), k,
+        _arg(out.get("logprob"), _F32T, n, "logprob"),
+        _arg(out.get("entropy"), _F32T, n, "entropy"), _arg(out.get("lse"), _F32T, n, "lse"),
+        _arg(out.get("stats"), _F32T, 2 * n, "stats"),
+        _arg(out.get("top_ids"), _I32T, n * k, "top_ids") if k else None,
+        _arg(out.get("top_logprob"), _F32T, n * k, "top_logprob") if k else None,
+        _arg(status, _I32T, 1, "status"), _stream(stream))
+    _check(st, "pace_logits_logprob")
+    return out
+
+
+def logits_logprob_backward(lg: PaceLogits, targets, stats, dlp, entropy=None, dentropy=None,
+                            temperature=1.0, grad=None, status=None, stream=None):
+    """pace_logits_logprob_backward: the gradient [n_rows, V] in the logits' dtype.  grad
+    may be the logits tensor itself."""
+    logits = lg._keep[0]
+    n = lg.n_rows
+    if grad is None:
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    g_ptr, g_stride = _rows_arg(grad, (logits.dtype,), logits.shape, "grad")
+    st = lib().pace_logits_logprob_backward(
+        ctypes.byref(lg), _arg(targets, _I32T, n, "targets"), float(temperature),
+        _arg(stats, _F32T, 2 * n, "stats"), _arg(entropy, _F32T, n, "entropy"),
+        _arg(dlp, _F32T, n, "dlp"), _arg(dentropy, _F32T, n, "dentropy"), g_ptr, g_stride,
+        _arg(status, _I32T, 1, "status"), _stream(stream))
+    _check(st, "pace_logits_logprob_backward")
+    return grad

@@ -1,0 +1,431 @@
+"""Log-probs, entropy and alternatives from logits in memory, and their gradient, against a
+plain statement of the formulas in 64 bits (torch, CPU).
+
+Tolerances, for float32 sums of up to V terms a row: a term's exponent is rounded to 2^-24
+of itself and its exponential to 2^-22, so a term is off by at most 2^-22 + |d2| 2^-23 of
+itself, and terms below 2^-40 of the largest do not count: 5e-6.  Adding up at most V / 32
+terms in a lane and 8 partial sums adds (V / 32 + 16) 2^-24 at worst and its square root as a
+rule; 1e-5 covers both for V up to 200,000 (a lane has at most V / 256 of them there).  So
+ln S is within 1e-5; lp adds three roundings of (z_y - m) / t; the entropy's second term is a
+quotient of two such sums, within 2e-5 of itself.  Places are compared exactly."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_36830_gb300 import pace
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+SUM = 1e-5
+EPS = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+INF = math.inf
+
+
+def reference(z, targets, t, k, allowed=None):
+    """(logprob, lse, entropy, ids, top, p, lp) in 64 bits of the values in z [R, V]."""
+    z = z.double().cpu().clone()
+    if allowed is not None:
+        z[~allowed] = -INF
+    m = z.amax(1, keepdim=True)
+    empty = m == -INF
+    d = (z - torch.where(empty, 0 * m.nan_to_num(), m)) / t
+    e = torch.exp(d)
+    s = e.sum(1, keepdim=True)
+    lp = torch.where(empty, torch.full_like(d, -INF), d - torch.log(s))
+    p = torch.exp(lp)
+    ent = -torch.where(p > 0, p * lp, 0 * p).sum(1)
+    lse = torch.where(empty[:, 0], torch.full_like(s[:, 0], -INF), (m / t)[:, 0] + torch.log(s)[:, 0])
+    # by value, equal ones lowest place first: a stable sort of the negated values
+    order = torch.sort(-(z + 0.0), dim=1, stable=True).indices[:, :k]
+    if order.shape[1] < k:
+        order = torch.cat([order, torch.zeros(z.shape[0], k - order.shape[1],
+                                              dtype=torch.int64)], 1)
+        there = torch.gather(z, 1, order) > -INF
+        there[:, z.shape[1]:] = False
+    else:
+        there = torch.gather(z, 1, order) > -INF
+    ids = torch.where(there, order, -torch.ones_like(order))
+    top = torch.where(there, torch.gather(lp, 1, order), torch.full_like(order, -INF, dtype=torch.float64))
+    y = targets.long().cpu()
+    return lp.gather(1, y[:, None])[:, 0], lse, ent, ids, top, p, lp
+
+
+def pack_bits(allowed):
+    R, V = allowed.shape
+    words = (V + 31) // 32
+    a = np.zeros((R, words * 32), np.uint8)
+    a[:, :V] = allowed.numpy()
+    return torch.from_numpy(np.packbits(a, axis=1, bitorder="little").view(np.int32).copy())
+
+
+def close(got, want, tol, what):
+    got, want = got.double().cpu(), want.double()
+    want = torch.where(want.float().isinf(), want.float().double(), want)  # beyond float32
+    same = (got == want) | (got.isnan() & want.isnan())
+    bad = ~same & ~((got - want).abs() <= tol)
+    assert not bad.any(), (what, int(bad.sum()), got[bad][:4], want[bad][:4])
+
+
+def check_forward(z, t=1.0, k=0, allowed=None, seed=0, status_want=0, targets=None):
+    R, V = z.shape
+    g = torch.Generator().manual_seed(seed)
+    if targets is None:
+        targets = torch.randint(0, V, (R,), generator=g, dtype=torch.int32)
+    lg = pace.make_logits(z, None if allowed is None else pack_bits(allowed).to(DEV))
+    status = pace.new_status(DEV)
+    o = pace.logits_logprob(lg, targets.to(DEV), t, k, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == status_want
+    lp, lse, ent, ids, top, _, _ = reference(z, targets, t, k, allowed)
+    close(o["lse"], lse, SUM + 3 * 2.0 ** -24 * lse.abs().nan_to_num(posinf=0, neginf=0), "lse")
+    close(o["logprob"], lp, SUM + 3 * 2.0 ** -23 * lp.abs().nan_to_num(neginf=0), "logprob")
+    close(o["entropy"], ent, SUM + 2 * SUM * ent.abs(), "entropy")
+    if k:
+        assert torch.equal(o["top_ids"].cpu().long(), ids), (o["top_ids"].cpu() - ids).nonzero()[:4]
+        close(o["top_logprob"], top, SUM + 3 * 2.0 ** -23 * top.abs().nan_to_num(neginf=0), "top")
+    return o, targets
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("R,V,k", [(1, 1, 1), (1, 2, 5), (3, 7, 7), (2, 31, 64), (5, 33, 4),
+                                   (1, 255, 64), (4, 257, 20), (300, 500, 3), (2, 2048, 20),
+                                   (7, 4099, 64), (1, 50001, 20), (33, 50001, 5),
+                                   (700, 2049, 1), (2, 151936, 64), (13, 152064, 0)])
+def test_shapes(dtype, R, V, k):
+    g = torch.Generator().manual_seed(R + V)
+    z = (torch.randn(R, V, generator=g) * 3).to(dtype).to(DEV)
+    check_forward(z, 0.7, k)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("pad", [1, 3, 8, 61])
+def test_row_strides_and_offsets(dtype, pad):
+    """Rows that begin anywhere in a 16-byte vector, in a buffer whose padding is NaN."""
+    g = torch.Generator().manual_seed(pad)
+    R, V = 9, 5003
+    buf = torch.full((R, V + 2 * pad), math.nan, dtype=dtype)
+    buf[:, pad:pad + V] = (torch.randn(R, V, generator=g) * 3).to(dtype)
+    z = buf.to(DEV)[:, pad:pad + V]
+    check_forward(z, 1.3, 20)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("V,keep", [(100, 0.5), (4099, 0.03), (50001, 0.5), (50001, 1e-4)])
+def test_allowed_places(dtype, V, keep):
+    """Excluded places hold NaN and infinities; some rows have one place, some none."""
+    g = torch.Generator().manual_seed(V)
+    R = 11
+    allowed = torch.rand(R, V, generator=g) < keep
+    allowed[3] = False
+    allowed[4] = False
+    allowed[4, V - 1] = True
+    allowed[5] = False
+    allowed[5, 0] = True
+    z = torch.randn(R, V, generator=g) * 3
+    junk = torch.tensor([math.nan, INF, -INF])[torch.randint(0, 3, (R, V), generator=g)]
+    z = torch.where(allowed, z, junk).to(dtype).to(DEV)
+    o, _ = check_forward(z, 1.0, 20, allowed)
+    assert o["lse"][3].item() == -INF and o["entropy"][3].item() == 0.0
+    assert o["stats"][3, 0].item() == -INF and (o["top_ids"][3] == -1).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_lowest_values_and_infinities_as_masks(dtype):
+    """-inf and the type's lowest value: everything, everything but one, a stretch."""
+    V, low = 9001, torch.finfo(dtype).min
+    z = (torch.randn(8, V, generator=torch.Generator().manual_seed(3)) * 2).to(dtype)
+    z[0] = -INF
+    z[1] = low
+    z[2] = -INF
+    z[2, 8000] = -3.0
+    z[3] = low
+    z[3, 8000] = -3.0
+    z[4, 100:8900] = -INF
+    z[5, 100:8900] = low
+    z[6] = -INF
+    z[6, 17] = low
+    z[7] = low
+    z[7, ::2] = -INF
+    o, _ = check_forward(z.to(DEV), 0.7, 20)
+    assert abs(o["entropy"][1].item() - math.log(V)) < 1e-4
+    assert o["top_ids"][1].tolist() == list(range(20))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("R,V", [(1, 40000), (2, 151936), (400, 3001)])
+def test_ties_go_to_the_lowest_place(dtype, R, V):
+    g = torch.Generator().manual_seed(V)
+    flat = torch.zeros(R, V)
+    few = torch.randint(-2, 3, (R, V), generator=g).float()  # five values, signed zeros among them
+    few[few == 0] = torch.where(torch.rand(int((few == 0).sum()), generator=g) < 0.5, 0.0, -0.0)
+    rising = torch.arange(V).float().expand(R, V) / 8
+    falling = -rising
+    for z in (flat, few, rising, falling):
+        check_forward(z.to(dtype).contiguous().to(DEV), 1.0, 64)
+
+
+def test_nan_and_infinity_in_a_row_stay_in_it():
+    z = torch.randn(6, 3000, generator=torch.Generator().manual_seed(1))
+    z[1, 2999] = math.nan
+    z[4, 7] = INF
+    targets = torch.zeros(6, dtype=torch.int32, device=DEV)
+    status = pace.new_status(DEV)
+    o = pace.logits_logprob(pace.make_logits(z.to(DEV)), targets, 1.0, 4, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == pace.ERR_NAN_INPUT
+    for n in ("logprob", "lse", "entropy"):
+        assert o[n].isnan().tolist() == [False, True, False, False, True, False], n
+    assert (o["top_ids"][[1, 4]] == -1).all()
+    keep = [0, 2, 3, 5]
+    lp, lse, ent, ids, _, _, _ = reference(z[keep], targets[keep], 1.0, 4)
+    close(o["logprob"][keep], lp, 2 * SUM, "logprob")
+    assert torch.equal(o["top_ids"][keep].cpu().long(), ids)
+
+
+@pytest.mark.parametrize("V", [64, 50001])
+def test_masked_rows_are_not_read(V):
+    z = torch.randn(5, V, generator=torch.Generator().manual_seed(2))
+    z[1] = math.nan
+    mask = torch.tensor([1, 0, 1, 1, 0], dtype=torch.uint8, device=DEV)
+    targets = torch.tensor([0, -5, 3, 1, V], dtype=torch.int32, device=DEV)
+    status = pace.new_status(DEV)
+    o = pace.logits_logprob(pace.make_logits(z.to(DEV), mask=mask), targets, 1.0, 3, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    for n in ("logprob", "lse", "entropy"):
+        assert (o[n][[1, 4]] == 0).all() and o[n].isfinite().all()
+    assert (o["stats"][[1, 4]] == 0).all()
+    assert (o["top_ids"][[1, 4]] == -1).all() and (o["top_logprob"][[1, 4]] == -INF).all()
+
+
+def test_target_outside_the_vocabulary_is_reported():
+    z = torch.zeros(3, 10, device=DEV)
+    for bad in (-1, 10):
+        status = pace.new_status(DEV)
+        y = torch.tensor([0, bad, 9], dtype=torch.int32, device=DEV)
+        o = pace.logits_logprob(pace.make_logits(z), y, status=status)
+        torch.cuda.synchronize()
+        assert int(status.item()) == pace.ERR_INVALID_ARG
+        assert o["logprob"].isnan().tolist() == [False, True, False]
+        assert abs(o["lse"][1].item() - math.log(10)) < SUM
+
+
+def test_outputs_are_optional_and_rows_may_be_none():
+    z = torch.randn(4, 777, device=DEV)
+    whole = pace.logits_logprob(pace.make_logits(z), torch.zeros(4, dtype=torch.int32, device=DEV),
+                                top_k=3)
+    for n in ("entropy", "lse", "stats"):
+        one = pace.logits_logprob(pace.make_logits(z), out={n: torch.empty_like(whole[n])})
+        assert torch.equal(one[n], whole[n])
+    o = pace.logits_logprob(pace.make_logits(z[:0]), torch.zeros(0, dtype=torch.int32, device=DEV))
+    assert o["logprob"].numel() == 0
+
+
+def test_the_same_call_gives_the_same_bits():
+    z = (torch.randn(37, 50001, device=DEV) * 3).bfloat16()
+    y = torch.zeros(37, dtype=torch.int32, device=DEV)
+    a, b = (pace.logits_logprob(pace.make_logits(z), y, 0.9, 17) for _ in range(2))
+    for n in a:
+        assert torch.equal(a[n], b[n])
+
+
+def test_offsets_past_32_bits():
+    """The last rows of a buffer of 2.3 G logits."""
+    R, V = 15200, 152064
+    z = torch.zeros(R, V, dtype=torch.bfloat16, device=DEV)
+    last = (torch.randn(4, V, generator=torch.Generator().manual_seed(7)) * 3).bfloat16()
+    z[-4:] = last.to(DEV)
+    y = torch.full((R,), V - 1, dtype=torch.int32, device=DEV)
+    o = pace.logits_logprob(pace.make_logits(z), y, 1.0, 5)
+    lp, lse, ent, ids, _, _, _ = reference(last, y[-4:], 1.0, 5)
+    close(o["logprob"][-4:], lp, 2 * SUM, "logprob")
+    assert torch.equal(o["top_ids"][-4:].cpu().long(), ids)
+    assert (o["top_ids"][0].cpu() == torch.arange(5)).all()
+    dlp = torch.ones(R, device=DEV)
+    pace.logits_logprob_backward(pace.make_logits(z), y, o["stats"], dlp, grad=z)
+    _, _, _, _, _, p, _ = reference(last, y[-4:], 1.0, 5)
+    want = -p
+    want[:, V - 1] += 1
+    close(z[-4:], want, 2 * SUM * p + 2.0 ** -8 * want.abs(), "grad")
+
+
+def test_other_stream():
+    side = torch.cuda.Stream()
+    z = torch.randn(64, 50001, device=DEV)
+    y = torch.zeros(64, dtype=torch.int32, device=DEV)
+    want = pace.logits_logprob(pace.make_logits(z), y, top_k=5)
+    side.wait_stream(torch.cuda.current_stream())
+    out = pace.logits_logprob_outputs(64, 5, DEV)
+    with torch.cuda.stream(side):
+        z2 = z * 1.0
+        pace.logits_logprob(pace.make_logits(z2), y, top_k=5, out=out)
+    side.synchronize()
+    for n in want:
+        assert torch.equal(want[n], out[n])
+
+
+# ---------------------------------------------------------------- the gradient
+
+def check_backward(z, t=1.0, allowed=None, mask=None, entropy=True, grad=None, seed=0):
+    R, V = z.shape
+    g = torch.Generator().manual_seed(seed + 1)
+    y = torch.randint(0, V, (R,), generator=g, dtype=torch.int32)
+    dlp, dent = torch.randn(R, generator=g), torch.randn(R, generator=g)
+    before = z.clone()
+    lg = pace.make_logits(z, None if allowed is None else pack_bits(allowed).to(DEV),
+                          None if mask is None else mask.to(DEV))
+    status = pace.new_status(DEV)
+    o = pace.logits_logprob(lg, y.to(DEV), t, status=status)
+    got = pace.logits_logprob_backward(lg, y.to(DEV), o["stats"], dlp.to(DEV),
+                                       o["entropy"] if entropy else None,
+                                       dent.to(DEV) if entropy else None, t, grad=grad,
+                                       status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    _, _, ent, _, _, p, lp = reference(before, y, t, 0, allowed)
+    hot = torch.zeros_like(p).scatter_(1, y.long()[:, None], 1.0)
+    lp0 = torch.where(p > 0, lp, 0 * p)
+    e = dent.double()[:, None] if entropy else 0.0
+    want = (dlp.double()[:, None] * (hot - p) - e * p * (lp0 + ent[:, None])) / t
+    mag = (dlp.abs().double()[:, None] * p + abs(e) * p * (lp0.abs() + ent[:, None])) / t
+    out = before.double().cpu() == -INF
+    if allowed is not None:
+        out |= ~allowed
+    dead = out | out.all(1, keepdim=True)
+    if mask is not None:
+        dead |= (mask == 0)[:, None]
+    want[dead] = 0.0
+    mag[dead] = 0.0
+    # p and ln p within ln S's and the entropy's errors, then the type's rounding
+    tol = 4 * SUM * mag + 1.01 * EPS[z.dtype] * want.abs() + 2.0 ** -23 * dlp.abs()[:, None] * hot / t
+    if z.dtype == torch.float16:
+        tol = tol + 2.0 ** -25  # below the normal numbers
+    close(got, want, tol, "grad")
+    assert (got.cpu()[dead] == 0).all()
+    return got
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("R,V", [(1, 1), (3, 7), (5, 257), (2, 8193), (300, 500), (3, 50001)])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_gradient(dtype, R, V, entropy):
+    g = torch.Generator().manual_seed(R + V)
+    z = (torch.randn(R, V, generator=g) * 2).to(dtype).to(DEV)
+    check_backward(z, 0.7, entropy=entropy)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gradient_of_excluded_places_and_rows(dtype):
+    g = torch.Generator().manual_seed(5)
+    R, V = 12, 5003
+    allowed = torch.rand(R, V, generator=g) < 0.3
+    allowed[2] = False
+    mask = torch.ones(R, dtype=torch.uint8)
+    mask[7] = 0
+    z = torch.randn(R, V, generator=g) * 2
+    z = torch.where(allowed, z, torch.full_like(z, math.nan))
+    z[9, 100:4000] = -INF
+    z[7] = math.nan
+    allowed[9, 200] = True
+    z[10] = torch.finfo(dtype).min  # the row's own lowest value everywhere
+    check_backward(z.to(dtype).to(DEV), 1.3, allowed=allowed, mask=mask)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("pad_z,pad_g", [(0, 3), (3, 0), (1, 8), (61, 61)])
+def test_gradient_strides(dtype, pad_z, pad_g):
+    R, V = 7, 4099
+    zb = (torch.randn(R, V + pad_z, device=DEV) * 2).to(dtype)
+    gb = torch.full((R, V + pad_g), 7.0, dtype=dtype, device=DEV)
+    allowed = torch.rand(R, V) < 0.5
+    check_backward(zb[:, :V], 1.0, allowed=allowed, grad=gb[:, :V])
+    assert (gb[:, V:] == 7.0).all()  # nothing beside the rows is written
+
+
+def test_gradient_in_place():
+    z = (torch.randn(9, 5001, device=DEV) * 2).bfloat16()
+    fresh = check_backward(z.clone(), 1.0)
+    again = z.clone()
+    got = check_backward(again, 1.0, grad=again)
+    assert torch.equal(got, fresh)
+
+
+def test_gradient_against_differences():
+    """The gradient along a direction against the forward's own difference quotient.  A
+    row's sum f has f64 inputs of fp32 rounding 1e-5 (above), so with a step h the quotient
+    is off by 4e-5 / h plus h^2 / 6 of the third derivative, below |v|^3 here."""
+    R, V, h, t = 4, 300, 0.02, 0.8
+    g = torch.Generator().manual_seed(11)
+    z = torch.randn(R, V, generator=g).to(DEV)
+    v = torch.randn(R, V, generator=g).to(DEV)
+    v /= v.norm(dim=1, keepdim=True)
+    y = torch.randint(0, V, (R,), generator=g, dtype=torch.int32).to(DEV)
+    one, w = torch.ones(R, device=DEV), torch.full((R,), 0.5, device=DEV)
+
+    def f(x):
+        o = pace.logits_logprob(pace.make_logits(x), y, t)
+        return (o["logprob"] + 0.5 * o["entropy"]).double()
+    o = pace.logits_logprob(pace.make_logits(z), y, t)
+    grad = pace.logits_logprob_backward(pace.make_logits(z), y, o["stats"], one, o["entropy"], w, t)
+    slope = (grad.double() * v.double()).sum(1)
+    quotient = (f(z + h * v) - f(z - h * v)) / (2 * h)
+    assert (slope - quotient).abs().max().item() <= 4e-5 / h + h * h / 6 / t ** 3
+
+
+# ---------------------------------------------------------------- refusals
+
+def test_refusals():
+    z = torch.zeros(4, 100, device=DEV)
+    y = torch.zeros(4, dtype=torch.int32, device=DEV)
+    with pytest.raises(ValueError, match="contiguous rows"):
+        pace.make_logits(torch.zeros(100, 4, device=DEV).t())
+    with pytest.raises(ValueError, match="float64"):
+        pace.make_logits(z.double())
+    with pytest.raises(ValueError, match="overlap"):
+        pace.make_logits(z[:1].expand(4, 100))
+    with pytest.raises(ValueError, match="allowed"):
+        pace.make_logits(z, allowed=torch.zeros(4, 3, dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError, match="at least 4"):
+        pace.make_logits(z, mask=torch.ones(3, dtype=torch.uint8, device=DEV))
+    lg = pace.make_logits(z)
+    with pytest.raises(ValueError, match="int32"):
+        pace.logits_logprob(lg, y.long())
+    for t in (0.0, -1.0, math.inf, math.nan, 1e-42):
+        with pytest.raises(pace.PaceError) as e:
+            pace.logits_logprob(lg, y, t)
+        assert e.value.status == pace.ERR_INVALID_ARG
+    for k, st in ((-1, pace.ERR_INVALID_ARG), (65, pace.ERR_UNSUPPORTED_SHAPE)):
+        with pytest.raises(pace.PaceError) as e:
+            pace.logits_logprob(lg, y, top_k=k, out={"lse": torch.empty(4, device=DEV)})
+        assert e.value.status == st
+    with pytest.raises(ValueError, match="shape"):
+        pace.logits_logprob_backward(lg, y, torch.zeros(4, 2, device=DEV), torch.zeros(4, device=DEV),
+                                     grad=torch.zeros(4, 99, device=DEV))
+    with pytest.raises(ValueError, match="float32"):
+        pace.logits_logprob_backward(lg, y, torch.zeros(4, 2, device=DEV), torch.zeros(4, device=DEV),
+                                     grad=torch.zeros(4, 100, device=DEV).bfloat16())
+
+
+def test_refusals_of_the_library_need_no_gpu_work():
+    L, fake = pace.lib(), 0x1000
+    good = dict(logits=fake, dtype=1, vocab_size=100, n_rows=4, row_stride=100, allowed=None,
+                allowed_stride=0, mask=None)
+
+    def call(**kw):
+        lg = pace.PaceLogits(*({**good, **kw}[n] for n, _ in pace.PaceLogits._fields_))
+        return L.pace_logits_logprob(ctypes.byref(lg), fake, 1.0, 0, fake, None, None, None, None,
+                                     None, None, None)
+    assert call(dtype=3) == pace.ERR_INVALID_ARG
+    assert call(n_rows=-1) == pace.ERR_INVALID_ARG
+    assert call(row_stride=99) == pace.ERR_INVALID_ARG
+    assert call(logits=None) == pace.ERR_INVALID_ARG
+    assert call(vocab_size=0) == pace.ERR_UNSUPPORTED_SHAPE
+    assert call(vocab_size=(1 << 24) + 1, row_stride=1 << 25) == pace.ERR_UNSUPPORTED_SHAPE
+    assert call(n_rows=(1 << 28) + 1) == pace.ERR_UNSUPPORTED_SHAPE
+    assert call(logits=fake + 1) == pace.ERR_UNSUPPORTED_SHAPE
+    assert call(allowed=fake, allowed_stride=3) == pace.ERR_INVALID_ARG
+    assert L.pace_logits_logprob(None, fake, 1.0, 0, fake, None, None, None, None, None, None,
+                                 None) == pace.ERR_INVALID_ARG
