@@ -534,6 +534,46 @@ PACE_API size_t pace_token_logprob_backward_workspace_size(int64_t n_rows, int64
                                                            int32_t vocab_size);
 
 /* ------------------------------------------------------------------------ */
+/* Entropy of the policy through the fused LM head                           */
+/* ------------------------------------------------------------------------ */
+
+/* pace_token_logprob with each row's entropy beside its log-prob, from the same
+ * pass over the vocabulary: with p = softmax(z / temperature),
+ *   entropy = -sum_v p_v ln p_v
+ * computed as ln S - T / S over exponentials against the running maximum (both
+ * terms are >= 0).  entropy is device float32 [n_rows], 0 outside the loss; the
+ * other arguments, outputs and errors are pace_token_logprob's (logprob and lse
+ * agree with it to the rounding of float32 sums taken in another order). */
+PACE_API pace_status pace_token_logprob_entropy(
+    const PaceBatch* batch, const void* hidden, const void* w_vocab, const int32_t* targets,
+    int32_t hidden_size, int32_t vocab_size, float temperature, float* logprob, float* lse,
+    float* entropy, const PaceLossArgs* loss, void* workspace, size_t workspace_bytes,
+    int32_t* status_dev, void* stream);
+
+PACE_API size_t pace_token_logprob_entropy_workspace_size(int64_t n_rows, int64_t n_seq,
+                                                          int32_t hidden_size,
+                                                          int32_t vocab_size);
+
+/* Its backward: gradients of sum_r dlp_r logprob_r + dentropy_r entropy_r, with
+ *   G_rv = (dlp_r / t) (1[v = y_r] - p_rv) - (dentropy_r / t) p_rv (ln p_rv + entropy_r)
+ * in place of pace_token_logprob_backward's G (held in bf16 like it).
+ *   lse, entropy  the forward's; entropy may be NULL when dentropy is.
+ *   dlp         device float32 [n_rows]; dentropy the same or NULL (0).
+ *   grad_dtype  PACE_F32, or PACE_BF16 for gradients rounded once from float32 sums
+ *               (of all rows: with more than 32,768 the workspace holds a float32 dW).
+ *   grad_hidden [n_rows][H], grad_w [V][H], device, of grad_dtype, 16-byte aligned.
+ * Other arguments and errors as for pace_token_logprob_backward. */
+PACE_API pace_status pace_token_logprob_entropy_backward(
+    const PaceBatch* batch, const void* hidden, const void* w_vocab, const int32_t* targets,
+    int32_t hidden_size, int32_t vocab_size, float temperature, const float* lse,
+    const float* entropy, const float* dlp, const float* dentropy, int32_t grad_dtype,
+    void* grad_hidden, void* grad_w, void* workspace, size_t workspace_bytes,
+    int32_t* status_dev, void* stream);
+
+PACE_API size_t pace_token_logprob_entropy_backward_workspace_size(
+    int64_t n_rows, int64_t n_seq, int32_t hidden_size, int32_t vocab_size, int32_t grad_dtype);
+
+/* ------------------------------------------------------------------------ */
 /* Log-probabilities, entropy and alternatives from logits in memory         */
 /* ------------------------------------------------------------------------ */
 

@@ -69,7 +69,8 @@ constexpr int kPaceSteps = 4096;
 constexpr int kMaxKSplits = 8;                // parts a tail tile is split into at most
 constexpr int kMaxGemmClusters = 76;          // clusters launched at most (bounds the partial tiles)
 
-enum { EPI_G = 0, EPI_ROWS = 1, EPI_ACC = 2 };
+// The epilogues; EPI_G_ENT adds the entropies' gradient to G, the two with 16 write bf16.
+enum { EPI_G = 0, EPI_ROWS = 1, EPI_ACC = 2, EPI_G_ENT = 3, EPI_ROWS16 = 4, EPI_ACC16 = 5 };
 enum { TRIM_NONE = 0, TRIM_M = 1, TRIM_K = 2 };
 
 struct GemmArgs {
@@ -85,6 +86,8 @@ struct GemmArgs {
   const int32_t* targets;
   const float* lse;             // forward log-sum-exp per original row
   const float* dlp;             // dLoss/dlp per original row
+  const float* entropy;         // EPI_G_ENT: the forward's entropy and dLoss/dentropy per
+  const float* dent;            // original row
   float scale_log2;             // log2(e) / tau
   float inv_tau;
   int64_t g_cols;               // bf16 G in 64-column blocks [g_cols / 64][g_pitch][64]: V rounded
@@ -94,12 +97,12 @@ struct GemmArgs {
   int64_t a_pitch;
   int32_t V;
   // EPI_ROWS
-  float* rows_out;              // fp32 [orig rows][ldo]
+  void* rows_out;               // fp32 (EPI_ROWS16: bf16) [orig rows][ldo]
   int64_t ldo;
   // partial tiles of the tail, or null: fp32 [part * items + item][2 GBM][GBN]
   float* part;
   // EPI_ACC
-  float* acc_out;               // fp32 [M][ldo]
+  void* acc_out;                // fp32 (EPI_ACC16: bf16, stored) [M][ldo]
   int acc_first;                // 1: store (the first chunk), 0: add
   unsigned* round_ctr;          // pacing counter, zeroed before the launch (or null)
   int32_t* status;
@@ -194,6 +197,9 @@ template <bool A_MN, bool B_MN, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
                 const __grid_constant__ CUtensorMap tm_c, GemmArgs p) {
+  constexpr bool kIsG = EPI == EPI_G || EPI == EPI_G_ENT;
+  constexpr bool kIsRows = EPI == EPI_ROWS || EPI == EPI_ROWS16;
+  constexpr bool kIsAcc = EPI == EPI_ACC || EPI == EPI_ACC16;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -232,14 +238,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
   const int nkb_all = static_cast<int>((K + GBK - 1) / GBK);
   // uniform over the grid, and before the pair's collective TMEM allocation
   if (nkb_all == 0 || base_items == 0) {
-    if (EPI == EPI_ACC && p.acc_first)  // no rows in the loss: dW = 0
+    if (kIsAcc && p.acc_first)  // no rows in the loss: dW = 0
       for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-           i < p.M * p.N / 4; i += static_cast<int64_t>(gridDim.x) * blockDim.x)
+           i < p.M * p.N / (EPI == EPI_ACC16 ? 8 : 4); i += static_cast<int64_t>(gridDim.x) * blockDim.x)
         reinterpret_cast<float4*>(p.acc_out)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     return;
   }
   TailSplit ts{base_items, 0, 1};
-  if (EPI == EPI_ROWS && p.part)
+  if (kIsRows && p.part)
     ts = tail_split(base_items, static_cast<int>(n_clusters), nkb_all);
   const int64_t n_items = ts.splits > 1 ? ts.full + static_cast<int64_t>(ts.tail) * ts.splits
                                         : base_items;
@@ -248,7 +254,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
     *k0 = 0;
     *k1 = nkb_all;
     *part = -1;
-    if (EPI != EPI_ROWS || ts.splits == 1 || t < ts.full) return t;
+    if (!kIsRows || ts.splits == 1 || t < ts.full) return t;
     const int u = static_cast<int>(t - ts.full);
     *part = u / ts.tail;
     *k0 = nkb_all * *part / ts.splits;
@@ -459,18 +465,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
       // per-row context
       bool row_ok = row < M;
       int32_t y = -1;
-      float gscale = 0.0f, lse2 = 0.0f;
+      float gscale = 0.0f, lse2 = 0.0f, escale = 0.0f, ent = 0.0f;
       int64_t orig = -1;
-      if (EPI == EPI_G || EPI == EPI_ROWS) {
+      if (kIsG || kIsRows) {
         const int64_t crow = p.chunk_row0 + row;
         const bool in_loss = row_ok && crow < static_cast<int64_t>(*p.n_valid);
         if (in_loss) orig = p.rowidx[crow];
-        if (EPI == EPI_G && in_loss) {
+        if (kIsG && in_loss) {
           y = p.targets[orig];
           gscale = p.dlp[orig] * p.inv_tau;
           lse2 = p.lse[orig] * 1.4426950408889634f;
+          if (EPI == EPI_G_ENT) {
+            escale = p.dent[orig] * p.inv_tau;
+            ent = p.entropy[orig];
+          }
         }
-        if (EPI == EPI_ROWS) row_ok = in_loss;
+        if (kIsRows) row_ok = in_loss;
       }
 #pragma unroll 1
       for (int c = 0; c < GBN; c += 32) {
@@ -478,20 +488,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
         tmem_ld_32x32b_x32(tbase + c, v);
         tmem_wait_ld();
         const int64_t col0 = n0 + c;
-        if (EPI == EPI_G) {
+        if (kIsG) {
           if (row_w < M && col0 < p.g_cols) {  // M is a multiple of 32: all its rows
             // G = (g / tau) (onehot - p), zero for rows outside the loss.  This epilogue
             // bounds the G GEMM at small H (a 256-column tile takes 5 us of MMAs at H
             // 1024), so per-column tests stay out of it: with them and rounding in
             // integer arithmetic, a chunk of 32k rows (H 1024, V 50,001) took 3.88 ms,
             // now 2.40; 8,248 rows 1.01 -> 0.62 ms; 2,582 rows of H 2048 1.08 -> 1.02.
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = ex2_approx(fmaf(v[i], p.scale_log2, -lse2));
             const uint32_t off = static_cast<uint32_t>(y - col0);
-            if (off < 32u) {  // the target: 1 - p, kept as -(1 - p) for the product below
+            if (EPI == EPI_G) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (off == static_cast<uint32_t>(i)) v[i] = -(1.0f - v[i]);
+              for (int i = 0; i < 32; ++i) v[i] = ex2_approx(fmaf(v[i], p.scale_log2, -lse2));
+              if (off < 32u) {  // the target: 1 - p, kept as -(1 - p) for the product below
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (off == static_cast<uint32_t>(i)) v[i] = -(1.0f - v[i]);
+              }
+            } else {
+              // p (g + e (ln p + H)) / tau, negated below; the target: less g / tau
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float d = fmaf(v[i], p.scale_log2, -lse2);  // log2 p
+                v[i] = ex2_approx(d) * fmaf(escale, fmaf(d, 0.69314718055994531f, ent), gscale);
+              }
+              if (off < 32u) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (off == static_cast<uint32_t>(i)) v[i] -= gscale;
+              }
             }
             if (col0 + 32 > p.V) {
 #pragma unroll
@@ -501,8 +525,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
             uint32_t packed[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const uint32_t g = bf16x2_rn(-gscale * v[2 * i], -gscale * v[2 * i + 1]);
-              packed[i] = gscale != 0.0f ? g : 0u;
+              if (EPI == EPI_G) {
+                const uint32_t g = bf16x2_rn(-gscale * v[2 * i], -gscale * v[2 * i + 1]);
+                packed[i] = gscale != 0.0f ? g : 0u;
+              } else {
+                const uint32_t g = bf16x2_rn(-v[2 * i], -v[2 * i + 1]);
+                packed[i] = gscale != 0.0f || escale != 0.0f ? g : 0u;
+              }
             }
             // two chunks of 32 columns make one 64-column block's 128-byte rows
             if ((c & 32) == 0) orow = out_begin();
@@ -514,15 +543,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
             if (c & 32)
               out_end(0, static_cast<int32_t>((col0 >> 6) * p.g_pitch + row_w));
           }
-        } else if (EPI == EPI_ROWS) {
+        } else if (kIsRows) {
           if (part >= 0) {  // a partial tile, whole (its rows outside the loss are not read)
             float4* d4 = reinterpret_cast<float4*>(
                 p.part + ((t - ts.full) * (2 * GBM) + crank * GBM + r_local) * GBN + c);
 #pragma unroll
             for (int q = 0; q < 8; ++q)
               d4[q] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+          } else if (EPI == EPI_ROWS16) {  // N is a multiple of 64: all 32 columns or none
+            if (row_ok && col0 < p.N) {
+              uint4* d4 = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.rows_out) +
+                                                   orig * p.ldo + col0);
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                d4[q] = make_uint4(bf16x2_rn(v[8 * q], v[8 * q + 1]),
+                                   bf16x2_rn(v[8 * q + 2], v[8 * q + 3]),
+                                   bf16x2_rn(v[8 * q + 4], v[8 * q + 5]),
+                                   bf16x2_rn(v[8 * q + 6], v[8 * q + 7]));
+            }
           } else if (row_ok) {
-            float* dst = p.rows_out + orig * p.ldo + col0;
+            float* dst = static_cast<float*>(p.rows_out) + orig * p.ldo + col0;
             if (col0 + 32 <= p.N) {
               float4* d4 = reinterpret_cast<float4*>(dst);
 #pragma unroll
@@ -535,7 +575,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
         } else {
           // N is a multiple of 64, so a chunk of 32 columns is inside or outside; rows
           // past M are clipped by the tensor map
-          if (p.acc_first) {
+          if (EPI == EPI_ACC16) {  // two chunks of 32 columns make one row of 128 bytes
+            if (row_w < M && col0 < p.N) {
+              if ((c & 32) == 0) orow = out_begin();
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                out_chunk(orow, (c & 32 ? 4 : 0) + q,
+                          make_uint4(bf16x2_rn(v[8 * q], v[8 * q + 1]),
+                                     bf16x2_rn(v[8 * q + 2], v[8 * q + 3]),
+                                     bf16x2_rn(v[8 * q + 4], v[8 * q + 5]),
+                                     bf16x2_rn(v[8 * q + 6], v[8 * q + 7])));
+              if (c & 32) out_end(static_cast<int32_t>(col0 - 32), static_cast<int32_t>(row_w));
+            }
+          } else if (p.acc_first) {
             if (row_w < M && col0 < p.N) {
               orow = out_begin();
 #pragma unroll
@@ -546,7 +598,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
               out_end(static_cast<int32_t>(col0), static_cast<int32_t>(row_w));
             }
           } else if (row_ok && col0 < p.N) {  // (a TMA reduction would flush subnormals)
-            float4* d4 = reinterpret_cast<float4*>(p.acc_out + row * p.ldo + col0);
+            float4* d4 =
+                reinterpret_cast<float4*>(static_cast<float*>(p.acc_out) + row * p.ldo + col0);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
               float4 o = d4[q];
@@ -581,6 +634,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 // Adds the partial tiles of the tail of a dH GEMM (the same geometry as the GEMM's,
 // from the same device-side count), part 0 first, and writes their rows in the loss:
 // a warp per row of 256 columns.
+template <bool kOut16>
 __global__ void __launch_bounds__(256)
     reduce_tail_kernel(GemmArgs p, int n_clusters) {
   int64_t v = static_cast<int64_t>(*p.n_valid) - p.chunk_row0;
@@ -597,7 +651,7 @@ __global__ void __launch_bounds__(256)
     item_of(p, m_tiles, ts.full + i, &mp, &nt);
     const int64_t row = mp * (2 * GBM) + r;
     if (row >= v) continue;
-    float* dst = p.rows_out + static_cast<int64_t>(p.rowidx[p.chunk_row0 + row]) * p.ldo;
+    const int64_t dst = static_cast<int64_t>(p.rowidx[p.chunk_row0 + row]) * p.ldo;
     const int64_t n0 = nt * GBN;
     for (int c = lane * 4; c < GBN && n0 + c < p.N; c += 128) {  // N is a multiple of 64
       float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -609,8 +663,22 @@ __global__ void __launch_bounds__(256)
         a.z += x.z;
         a.w += x.w;
       }
-      *reinterpret_cast<float4*>(dst + n0 + c) = a;
+      if (kOut16)
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.rows_out) + dst + n0 + c) =
+            make_uint2(bf16x2_rn(a.x, a.y), bf16x2_rn(a.z, a.w));
+      else
+        *reinterpret_cast<float4*>(static_cast<float*>(p.rows_out) + dst + n0 + c) = a;
     }
+  }
+}
+
+// A bf16 copy of n float32 values (n a multiple of 8).
+__global__ void to_bf16_kernel(const float4* __restrict__ in, uint4* __restrict__ out, int64_t n) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n / 8;
+       i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+    const float4 a = in[2 * i], b = in[2 * i + 1];
+    out[i] = make_uint4(bf16x2_rn(a.x, a.y), bf16x2_rn(a.z, a.w), bf16x2_rn(b.x, b.y),
+                        bf16x2_rn(b.z, b.w));
   }
 }
 
@@ -890,8 +958,8 @@ pace_status launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUte
   gemm_kernel<A_MN, B_MN, EPI><<<static_cast<unsigned>(grid), kGemmThreads, kGSmemBytes, st>>>(
       ta, tb, tc, a);
   PACE_TRY(last_launch_status());
-  if (EPI == EPI_ROWS && a.part) {
-    reduce_tail_kernel<<<static_cast<unsigned>(sm_count() * 4), 256, 0, st>>>(
+  if ((EPI == EPI_ROWS || EPI == EPI_ROWS16) && a.part) {
+    reduce_tail_kernel<EPI == EPI_ROWS16><<<static_cast<unsigned>(sm_count() * 4), 256, 0, st>>>(
         a, static_cast<int>(max_clusters));
     return last_launch_status();
   }
@@ -903,6 +971,7 @@ struct BwWs {
   uint16_t* g;        // bf16 G of one chunk, 64-column blocks [ceil(V / 64)][chunk][64]
   unsigned* round_ctr;  // the GEMMs' pacing counter
   float* part;          // dH's partial tiles
+  float* dw;            // bf16 gradients of several chunks: dW, added up in float32
 };
 
 int64_t chunk_rows(int64_t n_rows) {
@@ -910,7 +979,8 @@ int64_t chunk_rows(int64_t n_rows) {
   return (c + GBM - 1) / GBM * GBM;
 }
 
-void carve_bw_ws(Carver& cv, int64_t n_rows, int64_t n_seq, int H, int V, BwWs* w) {
+void carve_bw_ws(Carver& cv, int64_t n_rows, int64_t n_seq, int H, int V, BwWs* w,
+                 bool out16 = false) {
   carve_lm_ws(cv, n_rows, n_seq, H, true, &w->lm);
   const int64_t g_cols = (static_cast<int64_t>(V) + 63) / 64 * 64;
   w->g = cv.take<uint16_t>(static_cast<size_t>(chunk_rows(n_rows > 0 ? n_rows : 1)) * g_cols);
@@ -922,6 +992,7 @@ void carve_bw_ws(Carver& cv, int64_t n_rows, int64_t n_seq, int H, int V, BwWs* 
   const int64_t tail = tiles < kMaxGemmClusters ? tiles : kMaxGemmClusters - 1;
   const int parts = max_k_splits(static_cast<int>((V + GBK - 1) / GBK));
   w->part = parts > 1 ? cv.take<float>(static_cast<size_t>(tail) * parts * 2 * GBM * GBN) : nullptr;
+  w->dw = out16 && n_rows > kChunkRows ? cv.take<float>(static_cast<size_t>(V) * H) : nullptr;
 }
 
 }  // namespace
@@ -1024,11 +1095,18 @@ extern "C" size_t pace_token_logprob_backward_workspace_size(int64_t n_rows, int
   return cv.used;
 }
 
-extern "C" pace_status pace_token_logprob_backward(
-    const PaceBatch* batch, const void* hidden, const void* w_vocab, const int32_t* targets,
-    int32_t hidden_size, int32_t vocab_size, float temperature, const float* lse,
-    const float* dlp, float* grad_hidden, float* grad_w, void* workspace,
-    size_t workspace_bytes, int32_t* status_dev, void* stream) {
+namespace pace {
+namespace {
+
+// The backward of log-probs and, where dent is given, of entropies, with float32 or bf16
+// gradients.
+pace_status backward_call(const PaceBatch* batch, const void* hidden, const void* w_vocab,
+                          const int32_t* targets, int32_t hidden_size, int32_t vocab_size,
+                          float temperature, const float* lse, const float* entropy,
+                          const float* dlp, const float* dent, bool out16, void* grad_hidden,
+                          void* grad_w, void* workspace, size_t workspace_bytes,
+                          int32_t* status_dev, void* stream) {
+  const size_t elem = out16 ? 2 : 4;
   const int H = hidden_size, V = vocab_size;
   PACE_TRY(check_lm_args(batch, hidden, w_vocab, targets, H, V, temperature, dlp));
   if (batch->n_rows > 0 && (!lse || !grad_hidden || !grad_w)) return PACE_ERR_INVALID_ARG;
@@ -1036,17 +1114,18 @@ extern "C" pace_status pace_token_logprob_backward(
   if (!workspace || !aligned(workspace, 256)) return PACE_ERR_WORKSPACE;
   Carver cv(workspace, workspace_bytes);
   BwWs ws;
-  carve_bw_ws(cv, batch->n_rows, batch->n_seq, H, V, &ws);
+  carve_bw_ws(cv, batch->n_rows, batch->n_seq, H, V, &ws, out16);
   if (!cv.fits()) return PACE_ERR_WORKSPACE;
   cudaStream_t st = as_stream(stream);
   const int64_t n_rows = batch->n_rows;
   if (n_rows == 0) {
-    PACE_TRY_CUDA(cudaMemsetAsync(grad_w, 0, static_cast<size_t>(V) * H * 4, st));
+    PACE_TRY_CUDA(cudaMemsetAsync(grad_w, 0, static_cast<size_t>(V) * H * elem, st));
     return PACE_OK;
   }
-  PACE_TRY_CUDA(cudaMemsetAsync(grad_hidden, 0, static_cast<size_t>(n_rows) * H * 4, st));
+  PACE_TRY_CUDA(cudaMemsetAsync(grad_hidden, 0, static_cast<size_t>(n_rows) * H * elem, st));
   // the rows in the loss, gathered densely (always compacted here)
-  PACE_TRY(run_compaction(batch, ws.lm.cw, AdvJob{}, nullptr, nullptr, nullptr, nullptr, status_dev, st));
+  PACE_TRY(run_compaction(batch, ws.lm.cw, AdvJob{}, nullptr, nullptr, nullptr, nullptr, nullptr,
+                          status_dev, st));
   PACE_TRY(run_gather(hidden, H, n_rows, ws.lm.cw, ws.lm.hidden_c, st));
   const int64_t rows_cap = n_rows > 128 ? n_rows : 128;
   const int64_t row_vecs = static_cast<int64_t>(H) * 2 / 16;
@@ -1083,13 +1162,18 @@ extern "C" pace_status pace_token_logprob_backward(
       a.targets = targets;
       a.lse = lse;
       a.dlp = dlp;
+      a.entropy = entropy;
+      a.dent = dent;
       a.scale_log2 = 1.4426950408889634f / temperature;
       a.inv_tau = 1.0f / temperature;
       a.g_cols = g_cols;
       a.g_pitch = rows_c_pad;
       a.V = V;
       a.status = status_dev;
-      PACE_TRY((launch_gemm<false, false, EPI_G>(ta, tb, tc, a, ws.round_ctr, st)));
+      if (dent)
+        PACE_TRY((launch_gemm<false, false, EPI_G_ENT>(ta, tb, tc, a, ws.round_ctr, st)));
+      else
+        PACE_TRY((launch_gemm<false, false, EPI_G>(ta, tb, tc, a, ws.round_ctr, st)));
     }
     // 2. dH rows = G W   (W read MN-major: [K = V][N = H])
     {
@@ -1110,13 +1194,21 @@ extern "C" pace_status pace_token_logprob_backward(
       a.ldo = H;
       a.part = ws.part;
       a.status = status_dev;
-      PACE_TRY((launch_gemm<false, true, EPI_ROWS>(ta, tb, ta, a, ws.round_ctr, st)));
+      if (out16)
+        PACE_TRY((launch_gemm<false, true, EPI_ROWS16>(ta, tb, ta, a, ws.round_ctr, st)));
+      else
+        PACE_TRY((launch_gemm<false, true, EPI_ROWS>(ta, tb, ta, a, ws.round_ctr, st)));
     }
-    // 3. dW += G^T H_c   (G read MN-major: [K = rows][M = V]; H_c MN-major: [K = rows][N = H])
+    // 3. dW += G^T H_c, in float32 (a lone chunk's bf16 dW is stored as it is)   (G read MN-major: [K = rows][M = V]; H_c MN-major: [K = rows][N = H])
     {
       CUtensorMap ta, tb, tc;
       PACE_TRY(encode_bf16_2d(&ta, ws.g, g_blocks * rows_c_pad, 64, 64, 64, 64));
-      PACE_TRY(encode_f32_2d(&tc, grad_w, V, H, H, 32, 32));
+      void* dw = ws.dw ? ws.dw : grad_w;
+      const bool dw16 = out16 && !ws.dw;
+      if (dw16)
+        PACE_TRY(encode_bf16_2d(&tc, dw, V, H, H, 64, 32));
+      else
+        PACE_TRY(encode_f32_2d(&tc, dw, V, H, H, 32, 32));
       PACE_TRY(encode_bf16_2d(&tb, hc, hc_rows, H, H, 64, 64));
       GemmArgs a = {};
       a.M = V;
@@ -1127,12 +1219,59 @@ extern "C" pace_status pace_token_logprob_backward(
       a.trim = TRIM_K;
       a.chunk_row0 = c0;
       a.n_valid = ws.lm.cw.total;
-      a.acc_out = grad_w;
+      a.acc_out = dw;
       a.acc_first = c0 == 0 ? 1 : 0;
       a.ldo = H;
       a.status = status_dev;
-      PACE_TRY((launch_gemm<true, true, EPI_ACC>(ta, tb, tc, a, ws.round_ctr, st)));
+      if (dw16)
+        PACE_TRY((launch_gemm<true, true, EPI_ACC16>(ta, tb, tc, a, ws.round_ctr, st)));
+      else
+        PACE_TRY((launch_gemm<true, true, EPI_ACC>(ta, tb, tc, a, ws.round_ctr, st)));
     }
   }
+  if (ws.dw) {
+    to_bf16_kernel<<<static_cast<unsigned>(sm_count() * 8), 256, 0, st>>>(
+        reinterpret_cast<const float4*>(ws.dw), static_cast<uint4*>(grad_w),
+        static_cast<int64_t>(V) * H);
+    return last_launch_status();
+  }
   return PACE_OK;
+}
+
+}  // namespace
+}  // namespace pace
+
+extern "C" pace_status pace_token_logprob_backward(
+    const PaceBatch* batch, const void* hidden, const void* w_vocab, const int32_t* targets,
+    int32_t hidden_size, int32_t vocab_size, float temperature, const float* lse,
+    const float* dlp, float* grad_hidden, float* grad_w, void* workspace,
+    size_t workspace_bytes, int32_t* status_dev, void* stream) {
+  return backward_call(batch, hidden, w_vocab, targets, hidden_size, vocab_size, temperature, lse,
+                       nullptr, dlp, nullptr, false, grad_hidden, grad_w, workspace,
+                       workspace_bytes, status_dev, stream);
+}
+
+extern "C" size_t pace_token_logprob_entropy_backward_workspace_size(int64_t n_rows,
+                                                                     int64_t n_seq,
+                                                                     int32_t hidden_size,
+                                                                     int32_t vocab_size,
+                                                                     int32_t grad_dtype) {
+  if (n_rows < 0 || n_seq < 0 || hidden_size <= 0 || vocab_size <= 0) return 0;
+  Carver cv;
+  BwWs w;
+  carve_bw_ws(cv, n_rows, n_seq, hidden_size, vocab_size, &w, grad_dtype == PACE_BF16);
+  return cv.used;
+}
+
+extern "C" pace_status pace_token_logprob_entropy_backward(
+    const PaceBatch* batch, const void* hidden, const void* w_vocab, const int32_t* targets,
+    int32_t hidden_size, int32_t vocab_size, float temperature, const float* lse,
+    const float* entropy, const float* dlp, const float* dentropy, int32_t grad_dtype,
+    void* grad_hidden, void* grad_w, void* workspace, size_t workspace_bytes,
+    int32_t* status_dev, void* stream) {
+  if (grad_dtype != PACE_F32 && grad_dtype != PACE_BF16) return PACE_ERR_INVALID_ARG;
+  if (dentropy && !entropy) return PACE_ERR_INVALID_ARG;
+  return backward_call(batch, hidden, w_vocab, targets, hidden_size, vocab_size, temperature, lse,
+                       entropy, dlp, dentropy, grad_dtype == PACE_BF16, grad_hidden, grad_w,
+                       workspace, workspace_bytes, status_dev, stream);
 }

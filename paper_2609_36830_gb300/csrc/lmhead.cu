@@ -32,7 +32,10 @@
 //                     TMEM lane), reads its 256 logits 32 columns at a time
 //                     with tcgen05.ld, keeps a running base-2 max and sum of
 //                     exponentials (online log-sum-exp) and picks out the
-//                     target's logit.
+//                     target's logit.  For entropies (kEntropy) it also keeps
+//                     T = sum e d beside S = sum e, e = 2^d with d <= 0 the distance
+//                     to the running max: H = ln S - ln 2 T / S has no cancellation.
+//                     One fused multiply-add a logit more, behind the MMAs.
 // No operand is multicast: every CTA reads only its own tiles; the pair shares
 // the vocabulary tile through the 2-CTA MMA itself.
 // Work is cut in two (lm_plan, evaluated on the device from the rows actually
@@ -62,6 +65,7 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -239,6 +243,7 @@ struct LmArgs {
   int32_t max_level;            // largest box level no taller than the hidden-state tensor
   float* part_m;                // the rounds' rows: row r's splits at r * S; then the
   float* part_s;                // tail's rows, tail_slots each
+  float* part_t;                // kEntropy: sum of e d beside the sum of e, d in powers of two
   float* tgt_logit;             // [rows_cap]
   unsigned* round_ctr;          // pacing counter, zero at launch (or null: no pacing)
   int32_t* status;
@@ -394,7 +399,7 @@ __device__ void plan_block_loads(const int32_t* __restrict__ rowidx, int64_t row
   __syncwarp();
 }
 
-template <bool kFine>
+template <bool kFine, bool kEntropy>
 __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
     lmhead_lse_kernel(const __grid_constant__ AMaps<kFine> am, const __grid_constant__ CUtensorMap tm_b,
                       LmArgs p) {
@@ -632,8 +637,11 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
       int64_t row;
       bool row_ok, have_tgt;
       int32_t y;
-      float m, s, tgt;
+      float m, s, t, tgt;
     };
+    // Columns past the vocabulary: -inf, or where e d must stay finite, so far below
+    // every logit that e is 0.  Maxima start there too.
+    const float outside = kEntropy ? fmaxf(-1e30f / scale, -FLT_MAX) : -INFINITY;
     auto start_row = [&](int64_t rp, RowState& rs) {
       rs.row = (rp * CLUSTER + crank) * BM + r_local;
       rs.row_ok = rs.row < n_valid;
@@ -642,8 +650,9 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
         const int64_t orig = p.rowidx ? static_cast<int64_t>(p.rowidx[rs.row]) : rs.row;
         rs.y = p.targets[orig];
       }
-      rs.m = -INFINITY;
+      rs.m = kEntropy ? -1e30f : -INFINITY;
       rs.s = 0.0f;
+      rs.t = 0.0f;
       rs.tgt = 0.0f;
       rs.have_tgt = false;
     };
@@ -651,6 +660,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
       if (!rs.row_ok) return;
       p.part_m[o] = rs.m;
       p.part_s[o] = rs.s;
+      if (kEntropy) p.part_t[o] = rs.t;
       if (rs.have_tgt) p.tgt_logit[rs.row] = rs.tgt;
     };
     while (ok && seg.load()) {
@@ -678,6 +688,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t tbase = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + acc * BN;
         const int32_t y = which ? r1.y : r0.y;
         float m = which ? r1.m : r0.m, s = which ? r1.s : r0.s, tgt = which ? r1.tgt : r0.tgt;
+        float st = which ? r1.t : r0.t;
         bool have_tgt = which ? r1.have_tgt : r0.have_tgt;
 #pragma unroll 1
         for (int cc = 0; cc < BN; cc += 32) {
@@ -688,15 +699,27 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
           if (col0 + 32 > p.V) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (col0 + i >= p.V) v[i] = -INFINITY;
+              if (col0 + i >= p.V) v[i] = outside;
           }
           float cm = v[0];
 #pragma unroll
           for (int i = 1; i < 32; ++i) cm = fmaxf(cm, v[i]);
           const float m_new = fmaxf(m, cm * scale);
           float acc_s = 0.0f;
+          if (kEntropy) {
+            float acc_t = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) acc_s += ex2_approx(fmaf(v[i], scale, -m_new));
+            for (int i = 0; i < 32; ++i) {
+              const float d = fmaf(v[i], scale, -m_new);
+              const float e = ex2_approx(d);
+              acc_s += e;
+              acc_t = fmaf(e, d, acc_t);
+            }
+            st = fmaf(ex2_approx(m - m_new), fmaf(m - m_new, s, st), acc_t);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc_s += ex2_approx(fmaf(v[i], scale, -m_new));
+          }
           s = s * ex2_approx(m - m_new) + acc_s;
           m = m_new;
           const uint32_t off = static_cast<uint32_t>(y - col0);
@@ -715,11 +738,13 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
         if (which) {
           r1.m = m;
           r1.s = s;
+          r1.t = st;
           r1.tgt = tgt;
           r1.have_tgt = have_tgt;
         } else {
           r0.m = m;
           r0.s = s;
+          r0.t = st;
           r0.tgt = tgt;
           r0.have_tgt = have_tgt;
         }
@@ -769,13 +794,14 @@ __device__ __forceinline__ void add_with_error(float& sum, float& err, float x) 
   sum = t;
 }
 
+template <bool kEntropy>
 __global__ void __launch_bounds__(kMergeThreads)
     lse_merge_kernel(int64_t rows_cap, const long long* __restrict__ n_valid_dev, int lm_clusters,
                      int n_vtiles, int split_pref, int32_t V, float inv_temp,
                      const float* __restrict__ part_m, const float* __restrict__ part_s,
-                     const float* __restrict__ tgt_logit, const int32_t* __restrict__ targets,
+                     const float* __restrict__ part_t, const float* __restrict__ tgt_logit, const int32_t* __restrict__ targets,
                      const int32_t* __restrict__ rowidx, float* __restrict__ logprob,
-                     float* __restrict__ lse_out, int32_t* status) {
+                     float* __restrict__ lse_out, float* __restrict__ entropy, int32_t* status) {
   const unsigned full = 0xffffffffu;
   const int64_t n_valid = n_valid_dev ? static_cast<int64_t>(*n_valid_dev) : rows_cap;
   // how the LM head dealt these rows
@@ -804,12 +830,21 @@ __global__ void __launch_bounds__(kMergeThreads)
     for (int s = sub; s < splits; s += lanes) mm = fmaxf(mm, part_m[o + s]);
     for (int x = lanes >> 1; x > 0; x >>= 1) mm = fmaxf(mm, __shfl_xor_sync(full, mm, x));
     float ss = 0.0f, se = 0.0f;  // the sum and its additions' errors
-    for (int s = sub; s < splits; s += lanes)
-      add_with_error(ss, se, part_s[o + s] * ex2_approx(part_m[o + s] - mm));
+    float ts = 0.0f, te = 0.0f;  // the same of sum e d
+    for (int s = sub; s < splits; s += lanes) {
+      const float d = part_m[o + s] - mm, f = ex2_approx(d);
+      add_with_error(ss, se, part_s[o + s] * f);
+      if (kEntropy) add_with_error(ts, te, f * fmaf(d, part_s[o + s], part_t[o + s]));
+    }
     for (int x = lanes >> 1; x > 0; x >>= 1) {
       const float s2 = __shfl_xor_sync(full, ss, x);
       se = __fadd_rn(se, __shfl_xor_sync(full, se, x));
       add_with_error(ss, se, s2);
+      if (kEntropy) {
+        const float t2 = __shfl_xor_sync(full, ts, x);
+        te = __fadd_rn(te, __shfl_xor_sync(full, te, x));
+        add_with_error(ts, te, t2);
+      }
     }
     if (!valid || sub != 0) continue;
     const float lse = (mm + lg2_approx(__fadd_rn(ss, se))) * 0.69314718055994531f;
@@ -824,6 +859,10 @@ __global__ void __launch_bounds__(kMergeThreads)
     }
     logprob[orig] = lp;
     if (lse_out) lse_out[orig] = lse;
+    if (kEntropy) {
+      const float sum = __fadd_rn(ss, se);
+      entropy[orig] = (log2f(sum) - __fadd_rn(ts, te) / sum) * 0.69314718055994531f;
+    }
   }
 }
 
@@ -842,7 +881,7 @@ struct LmLaunch {
   CUtensorMap tm_b;
   unsigned grid;
 };
-template <bool kFine>
+template <bool kFine, bool kEntropy>
 pace_status launch_lmhead(const LmLaunch& l, LmArgs a, cudaStream_t st) {
   using B = Boxes<kFine>;
   AMaps<kFine> am;
@@ -859,8 +898,16 @@ pace_status launch_lmhead(const LmLaunch& l, LmArgs a, cudaStream_t st) {
       am.box[j] = am.box[max_level];
   }
   a.max_level = max_level;
-  lmhead_lse_kernel<kFine><<<l.grid, kThreads, kSmemBytes, st>>>(am, l.tm_b, a);
+  lmhead_lse_kernel<kFine, kEntropy><<<l.grid, kThreads, kSmemBytes, st>>>(am, l.tm_b, a);
   return last_launch_status();
+}
+
+template <bool kFine, bool kEntropy>
+pace_status allow_lm_smem() {
+  PACE_TRY_CUDA(cudaFuncSetAttribute(lmhead_lse_kernel<kFine, kEntropy>,
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(kSmemBytes)));
+  return PACE_OK;
 }
 
 // Dynamic shared memory opt-in and the number of 2-CTA clusters that can be
@@ -874,12 +921,10 @@ pace_status lm_launch_info(LmLaunchInfo* out) {
   if (dev < 0 || dev >= kMaxDevices) return PACE_ERR_CUDA;
   std::lock_guard<std::mutex> g(mu);
   if (info[dev].max_clusters == 0) {
-    PACE_TRY_CUDA(cudaFuncSetAttribute(lmhead_lse_kernel<false>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(kSmemBytes)));
-    PACE_TRY_CUDA(cudaFuncSetAttribute(lmhead_lse_kernel<true>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(kSmemBytes)));
+    PACE_TRY((allow_lm_smem<false, false>()));
+    PACE_TRY((allow_lm_smem<true, false>()));
+    PACE_TRY((allow_lm_smem<false, true>()));
+    PACE_TRY((allow_lm_smem<true, true>()));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(sm_count()), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -892,7 +937,8 @@ pace_status lm_launch_info(LmLaunchInfo* out) {
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, lmhead_lse_kernel<false>, &cfg) != cudaSuccess || n < 1)
+    if (cudaOccupancyMaxActiveClusters(&n, lmhead_lse_kernel<false, false>, &cfg) != cudaSuccess ||
+        n < 1)
       n = sm_count() / CLUSTER;
     info[dev].max_clusters = n < kMaxClusters ? n : kMaxClusters;
   }
@@ -903,7 +949,7 @@ pace_status lm_launch_info(LmLaunchInfo* out) {
 }  // namespace
 
 void carve_lm_ws(Carver& cv, int64_t n_rows, int64_t n_seq, int H, bool dense_rows,
-                 LmWs* w) {
+                 LmWs* w, bool entropy) {
   const int64_t rows_cap = n_rows > BM ? n_rows : BM;
   carve_compact_ws(cv, n_rows, &w->cw);
   carve_surrogate_ws(cv, n_rows, n_seq, &w->sw);
@@ -918,6 +964,7 @@ void carve_lm_ws(Carver& cv, int64_t n_rows, int64_t n_seq, int H, bool dense_ro
   w->part_s = cv.take<float>(parts);
   w->tgt = cv.take<float>(static_cast<size_t>(rows_cap));
   w->round_ctr = cv.take<unsigned>(1);
+  w->part_t = entropy ? cv.take<float>(parts) : nullptr;
 }
 
 bool lm_needs_compaction(const PaceBatch* b) {
@@ -937,13 +984,13 @@ pace_status check_lm_args(const PaceBatch* batch, const void* hidden, const void
   return PACE_OK;
 }
 
-// Compaction, fused LM head and merge: lp (and lse) for every row in
+// Compaction, fused LM head and merge: lp (and lse, and entropy) for every row in
 // the batch's loss, 0 elsewhere.  When the rows are compacted, the same launches also
 // compute the advantages of `adv` and clear `counter` (the caller does otherwise).
 pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* w_vocab,
                         const int32_t* targets, int H, int V, float temperature, float* logprob,
                         float* lse, const LmWs& ws, const AdvJob& adv, unsigned* counter,
-                        int32_t* status_dev, cudaStream_t st) {
+                        int32_t* status_dev, cudaStream_t st, float* entropy) {
   const int64_t n_rows = batch->n_rows;
   const bool compact = lm_needs_compaction(batch);
   const long long* n_valid_dev = nullptr;
@@ -951,7 +998,8 @@ pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* 
   int64_t rows_cap = n_rows;
   if (compact) {
     // the LM head reads the rows in the loss through rowidx (no dense copy)
-    PACE_TRY(run_compaction(batch, ws.cw, adv, counter, ws.round_ctr, logprob, lse, status_dev, st));
+    PACE_TRY(run_compaction(batch, ws.cw, adv, counter, ws.round_ctr, logprob, lse, entropy,
+                            status_dev, st));
     n_valid_dev = ws.cw.total;
     rowidx = ws.cw.rowidx;
     rows_cap = n_rows > BM ? n_rows : BM;
@@ -979,6 +1027,7 @@ pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* 
   a.gather = compact ? 1 : 0;
   a.part_m = ws.part_m;
   a.part_s = ws.part_s;
+  a.part_t = ws.part_t;
   a.tgt_logit = ws.tgt;
   a.round_ctr = ws.round_ctr;
   a.status = status_dev;
@@ -992,15 +1041,20 @@ pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* 
   if (pe.begin) PACE_TRY_CUDA(cudaEventRecord(pe.begin, st));
   const bool fine =
       compact && n_rows >= BM && 2.0 * H * V * static_cast<double>(n_rows) >= kFineFlops;
-  PACE_TRY(fine ? launch_lmhead<true>(l, a, st) : launch_lmhead<false>(l, a, st));
+  if (entropy)
+    PACE_TRY((fine ? launch_lmhead<true, true>(l, a, st) : launch_lmhead<false, true>(l, a, st)));
+  else
+    PACE_TRY((fine ? launch_lmhead<true, false>(l, a, st) : launch_lmhead<false, false>(l, a, st)));
   if (pe.end) PACE_TRY_CUDA(cudaEventRecord(pe.end, st));
   const int64_t per_block = kMergeThreads / kMergeLanes;
   int64_t mblocks = (rows_cap + per_block - 1) / per_block;
   const int64_t cap = static_cast<int64_t>(sm_count()) * 8;
   if (mblocks > cap) mblocks = cap;
-  lse_merge_kernel<<<static_cast<unsigned>(mblocks), kMergeThreads, 0, st>>>(
+  const auto merge = entropy ? lse_merge_kernel<true> : lse_merge_kernel<false>;
+  merge<<<static_cast<unsigned>(mblocks), kMergeThreads, 0, st>>>(
       rows_cap, n_valid_dev, static_cast<int>(clusters), n_vtiles, a.split_pref, V,
-      1.0f / temperature, ws.part_m, ws.part_s, ws.tgt, targets, rowidx, logprob, lse, status_dev);
+      1.0f / temperature, ws.part_m, ws.part_s, ws.part_t, ws.tgt, targets, rowidx, logprob, lse,
+      entropy, status_dev);
   return last_launch_status();
 }
 
@@ -1017,20 +1071,22 @@ extern "C" size_t pace_token_logprob_workspace_size(int64_t n_rows, int64_t n_se
   return cv.used;
 }
 
-extern "C" pace_status pace_token_logprob(const PaceBatch* batch, const void* hidden,
-                                          const void* w_vocab, const int32_t* targets,
-                                          int32_t hidden_size, int32_t vocab_size,
-                                          float temperature, float* logprob, float* lse,
-                                          const PaceLossArgs* loss, void* workspace,
-                                          size_t workspace_bytes, int32_t* status_dev,
-                                          void* stream) {
+namespace pace {
+namespace {
+
+// Log-probs, lse and entropies (or null), and the loss where it is asked for.
+pace_status logprob_call(const PaceBatch* batch, const void* hidden, const void* w_vocab,
+                         const int32_t* targets, int32_t hidden_size, int32_t vocab_size,
+                         float temperature, float* logprob, float* lse, float* entropy,
+                         const PaceLossArgs* loss, void* workspace, size_t workspace_bytes,
+                         int32_t* status_dev, void* stream) {
   PACE_TRY(check_lm_args(batch, hidden, w_vocab, targets, hidden_size, vocab_size, temperature,
                          logprob));
   if (loss) PACE_TRY(check_loss_args(batch, loss));
   if (!workspace || !aligned(workspace, 256)) return PACE_ERR_WORKSPACE;
   Carver cv(workspace, workspace_bytes);
   LmWs ws;
-  carve_lm_ws(cv, batch->n_rows, batch->n_seq, hidden_size, false, &ws);
+  carve_lm_ws(cv, batch->n_rows, batch->n_seq, hidden_size, false, &ws, entropy != nullptr);
   if (!cv.fits()) return PACE_ERR_WORKSPACE;
   cudaStream_t st = as_stream(stream);
   AdvJob adv{};
@@ -1039,9 +1095,44 @@ extern "C" pace_status pace_token_logprob(const PaceBatch* batch, const void* hi
                   loss->params.adv_eps, loss->params.std_unbiased,
                   loss->adv ? loss->adv : ws.sw.adv);
   PACE_TRY(run_logprob(batch, hidden, w_vocab, targets, hidden_size, vocab_size, temperature,
-                       logprob, lse, ws, adv, loss ? ws.sw.counter : nullptr, status_dev, st));
+                       logprob, lse, ws, adv, loss ? ws.sw.counter : nullptr, status_dev, st,
+                       entropy));
   if (loss)
     PACE_TRY(run_surrogate(batch, logprob, loss, ws.sw, lm_needs_compaction(batch), status_dev,
                            st));
   return PACE_OK;
+}
+
+}  // namespace
+}  // namespace pace
+
+extern "C" pace_status pace_token_logprob(const PaceBatch* batch, const void* hidden,
+                                          const void* w_vocab, const int32_t* targets,
+                                          int32_t hidden_size, int32_t vocab_size,
+                                          float temperature, float* logprob, float* lse,
+                                          const PaceLossArgs* loss, void* workspace,
+                                          size_t workspace_bytes, int32_t* status_dev,
+                                          void* stream) {
+  return logprob_call(batch, hidden, w_vocab, targets, hidden_size, vocab_size, temperature,
+                      logprob, lse, nullptr, loss, workspace, workspace_bytes, status_dev, stream);
+}
+
+extern "C" size_t pace_token_logprob_entropy_workspace_size(int64_t n_rows, int64_t n_seq,
+                                                            int32_t hidden_size,
+                                                            int32_t vocab_size) {
+  if (n_rows < 0 || n_seq < 0 || hidden_size <= 0 || vocab_size <= 0) return 0;
+  Carver cv;
+  LmWs w;
+  carve_lm_ws(cv, n_rows, n_seq, hidden_size, false, &w, true);
+  return cv.used;
+}
+
+extern "C" pace_status pace_token_logprob_entropy(
+    const PaceBatch* batch, const void* hidden, const void* w_vocab, const int32_t* targets,
+    int32_t hidden_size, int32_t vocab_size, float temperature, float* logprob, float* lse,
+    float* entropy, const PaceLossArgs* loss, void* workspace, size_t workspace_bytes,
+    int32_t* status_dev, void* stream) {
+  if (!entropy && batch && batch->n_rows > 0) return PACE_ERR_INVALID_ARG;
+  return logprob_call(batch, hidden, w_vocab, targets, hidden_size, vocab_size, temperature,
+                      logprob, lse, entropy, loss, workspace, workspace_bytes, status_dev, stream);
 }

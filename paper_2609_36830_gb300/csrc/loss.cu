@@ -620,11 +620,11 @@ __global__ void __launch_bounds__(kRowThreads)
   }
 }
 
-// A tile's rows in the loss (the lanes' bits) into the list from entry `before` on; lp
-// and lse (or null) of its other rows are set to 0.
+// A tile's rows in the loss (the lanes' bits) into the list from entry `before` on; lp, lse
+// and entropy (or null) of its other rows are set to 0.
 __device__ __forceinline__ void list_tile(int64_t t0, int64_t t1, unsigned in, long long& before,
                                           int32_t* __restrict__ rowidx, float* __restrict__ lp,
-                                          float* __restrict__ lse) {
+                                          float* __restrict__ lse, float* __restrict__ entropy) {
   const int lane = threadIdx.x & 31;
   // 32 rows at a time, lane l row l of them (held by lane l / 8 of four), so that the
   // warp's stores are consecutive
@@ -638,6 +638,7 @@ __device__ __forceinline__ void list_tile(int64_t t0, int64_t t1, unsigned in, l
     } else if (r < t1) {
       if (lp) lp[r] = 0.0f;
       if (lse) lse[r] = 0.0f;
+      if (entropy) entropy[r] = 0.0f;
     }
     before += __popc(bal);
   }
@@ -645,14 +646,15 @@ __device__ __forceinline__ void list_tile(int64_t t0, int64_t t1, unsigned in, l
 
 // The row indices of the rows in the loss, in row order; their number in *total.
 // Every block adds up the counts of the blocks before it itself (at most
-// kMaxRowBlocks of them), so there is no launch for a scan.  lp and lse (or null) of
-// rows outside the loss are set to 0 here.
+// kMaxRowBlocks of them), so there is no launch for a scan.  lp, lse and entropy (or
+// null) of rows outside the loss are set to 0 here.
 __global__ void __launch_bounds__(kRowThreads)
     write_rows_kernel(const int64_t* __restrict__ seq_offsets,
                       const uint8_t* __restrict__ seq_accepted, const uint8_t* __restrict__ mask,
                       int64_t n_seq, int64_t n_rows, RowGeom geom, bool vec, RowCounts counts,
                       int32_t* __restrict__ rowidx, long long* __restrict__ total,
-                      float* __restrict__ lp, float* __restrict__ lse) {
+                      float* __restrict__ lp, float* __restrict__ lse,
+                      float* __restrict__ entropy) {
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int64_t warp = static_cast<int64_t>(blockIdx.x) * kRowWarps + wid;
   const int64_t w0 = warp * geom.per_warp;
@@ -668,7 +670,7 @@ __global__ void __launch_bounds__(kRowThreads)
   before += __reduce_add_sync(0xffffffffu, wc);
   walk_rows_in_loss(seq_offsets, seq_accepted, mask, n_seq, n_rows, w0, w1, vec,
                     [&](int64_t t0, int64_t t1, unsigned in) {
-                      list_tile(t0, t1, in, before, rowidx, lp, lse);
+                      list_tile(t0, t1, in, before, rowidx, lp, lse, entropy);
                     });
 }
 
@@ -687,8 +689,8 @@ __global__ void __launch_bounds__(kFewThreads)
                          const uint8_t* __restrict__ mask, int64_t n_seq, int64_t n_rows,
                          int blocks, bool vec, int32_t* __restrict__ rowidx,
                          long long* __restrict__ total, float* __restrict__ lp,
-                         float* __restrict__ lse, AdvJob adv, unsigned* counter0,
-                         unsigned* counter1, int32_t* status) {
+                         float* __restrict__ lse, float* __restrict__ entropy, AdvJob adv,
+                         unsigned* counter0, unsigned* counter1, int32_t* status) {
   if (static_cast<int>(blockIdx.x) >= blocks) {
     adv_block_call(adv, blockIdx.x - blocks);
     return;
@@ -722,7 +724,7 @@ __global__ void __launch_bounds__(kFewThreads)
   if (b == blocks - 1 && wid == kFewWarps - 1 && lane == 0) *total = before + n_own;
   if (w < n_tiles) {
     const int64_t t0 = w * kRowTile;
-    list_tile(t0, tile_end(t0, n_rows), own, before, rowidx, lp, lse);
+    list_tile(t0, tile_end(t0, n_rows), own, before, rowidx, lp, lse, entropy);
   }
 }
 
@@ -769,12 +771,13 @@ pace_status launch_count_rows(const PaceBatch* b, RowCounts counts, unsigned lon
 
 pace_status run_compaction(const PaceBatch* b, const CompactWs& ws, const AdvJob& adv,
                            unsigned* counter0, unsigned* counter1, float* lp, float* lse,
-                           int32_t* status, cudaStream_t st) {
+                           float* entropy, int32_t* status, cudaStream_t st) {
   if (b->n_seq == 0 || b->n_rows == 0) {
     PACE_TRY_CUDA(cudaMemsetAsync(ws.total, 0, sizeof(long long), st));
     const size_t bytes = static_cast<size_t>(b->n_rows) * sizeof(float);
     if (lp && bytes) PACE_TRY_CUDA(cudaMemsetAsync(lp, 0, bytes, st));
     if (lse && bytes) PACE_TRY_CUDA(cudaMemsetAsync(lse, 0, bytes, st));
+    if (entropy && bytes) PACE_TRY_CUDA(cudaMemsetAsync(entropy, 0, bytes, st));
     if (counter1) PACE_TRY_CUDA(cudaMemsetAsync(counter1, 0, sizeof(unsigned), st));
     return launch_group_adv(adv, b, counter0, status, st);
   }
@@ -783,15 +786,15 @@ pace_status run_compaction(const PaceBatch* b, const CompactWs& ws, const AdvJob
                                         (kFewWarps * kRowTile));
     list_few_rows_kernel<<<static_cast<unsigned>(blocks + adv_blocks(adv, kFewThreads)), kFewThreads, 0, st>>>(
         b->seq_offsets, b->seq_accepted, b->mask, b->n_seq, b->n_rows, blocks,
-        aligned(b->mask, 8), ws.rowidx, ws.total, lp, lse, adv, counter0, counter1, status);
+        aligned(b->mask, 8), ws.rowidx, ws.total, lp, lse, entropy, adv, counter0, counter1,
+        status);
     return last_launch_status();
   }
   PACE_TRY(launch_count_rows(b, ws.counts, nullptr, nullptr, adv, counter0, counter1, status, st));
   const RowGeom g = row_geom(b->n_rows);
   write_rows_kernel<<<static_cast<unsigned>(g.blocks), kRowThreads, 0, st>>>(
       b->seq_offsets, b->seq_accepted, b->mask, b->n_seq, b->n_rows, g, aligned(b->mask, 8),
-      ws.counts, ws.rowidx,
-      ws.total, lp, lse);
+      ws.counts, ws.rowidx, ws.total, lp, lse, entropy);
   return last_launch_status();
 }
 

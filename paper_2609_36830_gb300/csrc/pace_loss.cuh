@@ -48,6 +48,7 @@ struct LmWs {
                    // only; null for the forward, whose LM head reads rows by index)
   float* part_m;
   float* part_s;
+  float* part_t;    // entropies: beside part_m and part_s (else null)
   float* tgt;
   unsigned* round_ctr;  // the LM head's pacing counter (items whose loads were issued)
 };
@@ -58,7 +59,7 @@ AdvJob adv_job(const float* reward, const uint8_t* accepted, int64_t n_seq, int 
 pace_status launch_group_adv(const AdvJob& j, const PaceBatch* b, unsigned* counter,
                              int32_t* status, cudaStream_t st);
 void carve_lm_ws(Carver& cv, int64_t n_rows, int64_t n_seq, int H, bool dense_rows,
-                 LmWs* w);
+                 LmWs* w, bool entropy = false);
 bool lm_needs_compaction(const PaceBatch* b);
 pace_status check_lm_args(const PaceBatch* batch, const void* hidden, const void* w_vocab,
                           const int32_t* targets, int H, int V, float temperature,
@@ -66,17 +67,17 @@ pace_status check_lm_args(const PaceBatch* batch, const void* hidden, const void
 pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* w_vocab,
                         const int32_t* targets, int H, int V, float temperature, float* logprob,
                         float* lse, const LmWs& ws, const AdvJob& adv, unsigned* counter,
-                        int32_t* status_dev, cudaStream_t st);
+                        int32_t* status_dev, cudaStream_t st, float* entropy = nullptr);
 void carve_compact_ws(Carver& cv, int64_t n_rows, CompactWs* w);
 pace_status check_batch(const PaceBatch* b);
 pace_status check_loss_args(const PaceBatch* b, const PaceLossArgs* l);
 pace_status run_surrogate(const PaceBatch* b, const float* logprob, const PaceLossArgs* l,
                           const SurrogateWs& ws, bool adv_done, int32_t* status, cudaStream_t st);
-// Counts the rows in the loss and lists them; clears counter0 and counter1 and lp /
-// lse of the rows outside the loss (any may be null), and computes the advantages.
+// Counts the rows in the loss and lists them; clears counter0 and counter1 and lp / lse /
+// entropy of the rows outside the loss (any may be null), and computes the advantages.
 pace_status run_compaction(const PaceBatch* b, const CompactWs& ws, const AdvJob& adv,
                            unsigned* counter0, unsigned* counter1, float* lp, float* lse,
-                           int32_t* status, cudaStream_t st);
+                           float* entropy, int32_t* status, cudaStream_t st);
 RowCounts carve_row_counts(Carver& cv, int64_t n_rows);
 pace_status launch_count_rows(const PaceBatch* b, RowCounts counts, unsigned long long* seq_in,
                               int* n_used, const AdvJob& adv, unsigned* counter0,

@@ -107,6 +107,12 @@ SIGNATURES = {
     "pace_token_logprob_backward": ([_P, _P, _P, _P, _I32, _I32, _F32, _P, _P, _P, _P, _P, _SZ,
                                      _P, _P], _I32),
     "pace_token_logprob_backward_workspace_size": ([_I64, _I64, _I32, _I32], _SZ),
+    "pace_token_logprob_entropy": ([_P, _P, _P, _P, _I32, _I32, _F32, _P, _P, _P, _P, _P, _SZ,
+                                    _P, _P], _I32),
+    "pace_token_logprob_entropy_workspace_size": ([_I64, _I64, _I32, _I32], _SZ),
+    "pace_token_logprob_entropy_backward": ([_P, _P, _P, _P, _I32, _I32, _F32, _P, _P, _P, _P,
+                                             _I32, _P, _P, _P, _SZ, _P, _P], _I32),
+    "pace_token_logprob_entropy_backward_workspace_size": ([_I64, _I64, _I32, _I32, _I32], _SZ),
     "pace_logits_logprob": ([_P, _P, _F32, _I32, _P, _P, _P, _P, _P, _P, _P, _P], _I32),
     "pace_logits_logprob_backward": ([_P, _P, _F32, _P, _P, _P, _P, _P, _I64, _P, _P], _I32),
     "pace_set_profile_events": ([_I32, _P, _P], _I32),
@@ -649,6 +655,75 @@ def token_logprob_backward(batch: PaceBatch, hidden, w_vocab, targets, lse, dlp,
                                            _arg(ws, _U8, None, "ws"), ws.numel(),
                                            _arg(status, _I32T, 1, "status"), _stream(stream))
     _check(st, "pace_token_logprob_backward")
+    return grad_hidden, grad_w
+
+
+# ---------------------------------------------------------------- entropy of the head
+
+def token_logprob_entropy_workspace_size(n_rows, n_seq, hidden, vocab):
+    return lib().pace_token_logprob_entropy_workspace_size(int(n_rows), int(n_seq), int(hidden),
+                                                           int(vocab))
+
+
+def token_logprob_entropy(batch: PaceBatch, hidden, w_vocab, targets, temperature=1.0, loss=None,
+                          logprob=None, lse=None, entropy=None, ws=None, status=None,
+                          stream=None):
+    """pace_token_logprob_entropy: (logprob, lse, entropy), float32 [n_rows].  hidden
+    [n_rows, H] and w_vocab [V, H] are bf16 tensors."""
+    H, V = _head_shapes(batch, hidden, w_vocab)
+    n_rows = batch.n_rows
+    dev = hidden.device
+    logprob, lse, entropy = (
+        torch.empty(n_rows, dtype=torch.float32, device=dev) if t is None else t
+        for t in (logprob, lse, entropy))
+    if ws is None:
+        ws = workspace(token_logprob_entropy_workspace_size(n_rows, batch.n_seq, H, V), dev)
+    st = lib().pace_token_logprob_entropy(
+        ctypes.byref(batch), _arg(hidden, _BF16, None, "hidden"),
+        _arg(w_vocab, _BF16, None, "w_vocab"), _arg(targets, _I32T, n_rows, "targets"), H, V,
+        float(temperature), _arg(logprob, _F32T, n_rows, "logprob"),
+        _arg(lse, _F32T, n_rows, "lse"), _arg(entropy, _F32T, n_rows, "entropy"),
+        ctypes.byref(loss) if loss is not None else None, _arg(ws, _U8, None, "ws"), ws.numel(),
+        _arg(status, _I32T, 1, "status"), _stream(stream))
+    _check(st, "pace_token_logprob_entropy")
+    return logprob, lse, entropy
+
+
+def token_logprob_entropy_backward_workspace_size(n_rows, n_seq, hidden, vocab,
+                                                  grad_dtype=torch.bfloat16):
+    return lib().pace_token_logprob_entropy_backward_workspace_size(
+        int(n_rows), int(n_seq), int(hidden), int(vocab), _DTYPES[grad_dtype])
+
+
+def token_logprob_entropy_backward(batch: PaceBatch, hidden, w_vocab, targets, lse, dlp,
+                                   entropy=None, dentropy=None, temperature=1.0,
+                                   grad_hidden=None, grad_w=None, grad_dtype=torch.bfloat16,
+                                   ws=None, status=None, stream=None):
+    """pace_token_logprob_entropy_backward: (grad_hidden [n_rows, H], grad_w [V, H]) in
+    grad_dtype (bf16 or float32), or in the given tensors' type."""
+    H, V = _head_shapes(batch, hidden, w_vocab)
+    n_rows = batch.n_rows
+    dev = hidden.device
+    given = grad_hidden if grad_hidden is not None else grad_w
+    dtype = grad_dtype if given is None else given.dtype
+    if dtype not in (_BF16, _F32T):
+        raise ValueError(f"gradients are bfloat16 or float32, not {dtype}")
+    if grad_hidden is None:
+        grad_hidden = torch.empty(n_rows, H, dtype=dtype, device=dev)
+    if grad_w is None:
+        grad_w = torch.empty(V, H, dtype=dtype, device=dev)
+    if ws is None:
+        ws = workspace(token_logprob_entropy_backward_workspace_size(n_rows, batch.n_seq, H, V,
+                                                                     dtype), dev)
+    st = lib().pace_token_logprob_entropy_backward(
+        ctypes.byref(batch), _arg(hidden, _BF16, None, "hidden"),
+        _arg(w_vocab, _BF16, None, "w_vocab"), _arg(targets, _I32T, n_rows, "targets"), H, V,
+        float(temperature), _arg(lse, _F32T, n_rows, "lse"),
+        _arg(entropy, _F32T, n_rows, "entropy"), _arg(dlp, _F32T, n_rows, "dlp"),
+        _arg(dentropy, _F32T, n_rows, "dentropy"), _DTYPES[dtype],
+        _arg(grad_hidden, dtype, n_rows * H, "grad_hidden"), _arg(grad_w, dtype, V * H, "grad_w"),
+        _arg(ws, _U8, None, "ws"), ws.numel(), _arg(status, _I32T, 1, "status"), _stream(stream))
+    _check(st, "pace_token_logprob_entropy_backward")
     return grad_hidden, grad_w
 
 

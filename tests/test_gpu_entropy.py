@@ -1,0 +1,233 @@
+"""Entropies through the fused LM head, and their gradient, against 64-bit torch.
+
+Forward.  A logit is a 32-bit sum of H products, within dz = 12 H 2^-24 (|z| < 12, the bound
+the log-prob tests use).  dH/dz_j = -p_j (ln p_j + H) and sum_j p_j |ln p_j + H| <= 2 ln V, so
+an entropy is within (1 + 2 ln V) dz of the exact one, plus 32 x 2^-22 for the exponentials and
+the logarithm.
+
+Backward.  G is rounded to bf16: 2^-8 of itself, with 2^-10 for everything in 32 bits as in
+the log-prob tests; where terms of G cancel, the 32-bit part is 2^-14 of the terms' sum.
+bf16 gradients are rounded once more: 2^-8 of the result."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2609_36830_gb300 import pace
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+ELEM = 2.0 ** -8 + 2.0 ** -10
+
+
+def make(rows, H, V, keep=1.0, seed=0, w_scale=2.0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(rows * 31 + H + V + seed)
+    h = torch.randn(rows, H, device=DEV, generator=g).to(torch.bfloat16)
+    w = (torch.randn(V, H, device=DEV, generator=g) * w_scale / math.sqrt(H)).to(torch.bfloat16)
+    y = torch.randint(0, V, (rows,), device=DEV, generator=g, dtype=torch.int32)
+    mask = None
+    if keep < 1.0:
+        mask = (torch.rand(rows, device=DEV, generator=g) < keep).to(torch.uint8)
+    b = pace.make_batch(torch.tensor([0, rows], dtype=torch.int64, device=DEV), rows, mask=mask)
+    inn = torch.ones(rows, dtype=torch.bool, device=DEV) if mask is None else mask > 0
+    return g, h, w, y, b, inn
+
+
+def exact(h, w, y, t):
+    z = h.double() @ w.double().T / t
+    lp = z - torch.logsumexp(z, 1)[:, None]
+    return lp, -(torch.exp(lp) * lp).sum(1)
+
+
+@pytest.mark.parametrize("rows,H,V,keep,t", [
+    (1, 64, 1, 1.0, 1.0), (1, 64, 2, 1.0, 1.0), (5, 64, 3, 1.0, 0.7), (8, 256, 2048, 1.0, 1.0),
+    (127, 64, 255, 1.0, 1.0), (128, 64, 256, 1.0, 1.3), (129, 192, 257, 0.5, 1.0),
+    (300, 1024, 4099, 0.7, 0.7), (2583, 128, 5000, 1.0, 1.0), (4864, 64, 1300, 1.0, 1.0),
+    (20001, 64, 600, 0.9, 1.0), (64, 64, 300, 0.0, 1.0), (600, 64, 50001, 0.5, 1.0)])
+def test_entropy(rows, H, V, keep, t):
+    _, h, w, y, b, inn = make(rows, H, V, keep)
+    status = pace.new_status(DEV)
+    lp, lse, ent = pace.token_logprob_entropy(b, h, w, y, t, status=status)
+    lse0 = torch.empty_like(lse)
+    lp0 = pace.token_logprob(b, h, w, y, t, lse=lse0)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    dz = 12 * H * 2.0 ** -24 / t
+    for a, c in ((lp, lp0), (lse, lse0)):  # as without entropies
+        assert ((a - c).abs() <= 2 * (2 * dz + 16 * 2.0 ** -22)).all()
+    exact_lp, want = exact(h, w, y, t)
+    exact_lp = exact_lp.gather(1, y.long()[:, None])[:, 0]
+    assert ((lp - exact_lp).abs()[inn] <= 2 * dz + 16 * 2.0 ** -22).all()
+    assert (lp[~inn] == 0).all() and (lse[~inn] == 0).all()
+    tol = dz * (1 + 2 * math.log(V)) + 32 * 2.0 ** -22
+    assert ((ent - want).abs()[inn] <= tol).all(), (ent - want).abs()[inn].max().item()
+    assert (ent[~inn] == 0).all()
+
+
+def test_uniform_and_certain_rows():
+    """W = 0: ln V.  A logit far above the rest: an entropy of a few e^-d, to the last bits
+    (ln S + T / S without cancellation)."""
+    h = torch.zeros(3, 64, dtype=torch.bfloat16, device=DEV)
+    h[:, 0] = torch.tensor([0.0, 16.0, 64.0])
+    V = 1000
+    w = torch.zeros(V, 64, dtype=torch.bfloat16, device=DEV)
+    w[17, 0] = 1.0
+    y = torch.full((3,), 17, dtype=torch.int32, device=DEV)
+    b = pace.make_batch(torch.tensor([0, 3], dtype=torch.int64, device=DEV), 3)
+    _, _, ent = pace.token_logprob_entropy(b, h, w, y)
+    _, want = exact(h, w, y, 1.0)
+    assert abs(ent[0].item() - math.log(V)) < 1e-5
+    assert abs(ent[1].item() - want[1].item()) < 1e-5 * want[1].item() + 2.0 ** -22
+    assert 0.0 <= ent[2].item() < 1e-20
+
+
+def test_loss_and_outputs_beside_entropy():
+    rows, H, V = 320, 64, 700
+    g, h, w, y, _, _ = make(rows, H, V)
+    b = pace.make_batch(torch.arange(0, rows + 1, 40, dtype=torch.int64, device=DEV), rows)
+    behav = torch.randn(rows, device=DEV, generator=g) - math.log(V)
+    reward = torch.rand(8, device=DEV, generator=g)
+    losses = []
+    for call in (pace.token_logprob, pace.token_logprob_entropy):
+        loss = torch.zeros(1, dtype=torch.float64, device=DEV)
+        la = pace.make_loss_args(behav, reward, 8, pace.loss_params(), loss)
+        call(b, h, w, y, 1.0, loss=la)
+        losses.append(loss.item())
+    assert abs(losses[0] - losses[1]) <= 1e-5 * abs(losses[0]) and losses[0] != 0.0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("entropy", [False, True])
+@pytest.mark.parametrize("rows,H,V,keep,t", [
+    (1, 64, 1, 1.0, 1.0), (3, 64, 7, 1.0, 0.7), (100, 64, 256, 1.0, 1.0), (300, 128, 1000, 0.6, 0.7),
+    (700, 192, 4099, 0.7, 1.0), (257, 64, 20000, 1.0, 1.0), (2600, 320, 8200, 0.9, 1.3),
+    (300, 128, 4097, 0.0, 1.0), (33000, 64, 600, 0.999, 1.0), (66000, 64, 256, 0.4, 1.0)])
+def test_gradient(rows, H, V, keep, t, entropy, dtype):
+    g, h, w, y, b, inn = make(rows, H, V, keep, seed=1)
+    d = torch.randn(rows, device=DEV, generator=g)
+    e = torch.randn(rows, device=DEV, generator=g)
+    d[::7] = 0.0
+    e[::5] = 0.0
+    lp, ent = exact(h, w, y, t)
+    lse = torch.logsumexp(h.double() @ w.double().T / t, 1).float()
+    gh = torch.full((rows, H), math.nan, device=DEV, dtype=dtype)
+    gw = torch.full((V, H), math.nan, device=DEV, dtype=dtype)
+    status = pace.new_status(DEV)
+    pace.token_logprob_entropy_backward(b, h, w, y, lse, d, ent.float() if entropy else None,
+                                        e if entropy else None, t, gh, gw, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    p = torch.exp(lp)
+    hot = torch.zeros_like(p).scatter_(1, y.long()[:, None], 1.0)
+    dd, ee = d.double()[:, None], e.double()[:, None] * (1.0 if entropy else 0.0)
+    G = (dd * (hot - p) - ee * p * (lp + ent[:, None])) / t
+    A = (dd.abs() * (hot + p) + ee.abs() * p * (lp.abs() + ent[:, None])) / t
+    G[~inn] = 0.0
+    A[~inn] = 0.0
+    bound = ELEM * G.abs() + 2.0 ** -14 * A
+    hd, wd = h.double(), w.double()
+    for got, ref, mag in ((gh, G @ wd, bound @ wd.abs()), (gw, G.T @ hd, bound.T @ hd.abs())):
+        assert torch.isfinite(got).all()
+        tol = mag + (2.0 ** -8 * ref.abs() if dtype == torch.bfloat16 else 0.0)
+        bad = (got.double() - ref).abs() > tol
+        assert not bad.any(), (int(bad.sum()), bad.nonzero()[:4])
+    assert (gh[~inn] == 0).all()
+
+
+def test_float32_gradients_without_entropy_have_the_log_prob_call_s_bits():
+    g, h, w, y, b, _ = make(700, 128, 3001, 0.8)
+    d = torch.randn(700, device=DEV, generator=g)
+    _, lse, _ = pace.token_logprob_entropy(b, h, w, y)
+    a = pace.token_logprob_backward(b, h, w, y, lse, d)
+    c = pace.token_logprob_entropy_backward(b, h, w, y, lse, d, grad_dtype=torch.float32)
+    assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+
+
+def test_gradient_against_differences():
+    """dH and dW along a direction against the forward's difference quotient.  f is a mean
+    over rows of lp + 0.3 H, within 1e-5 (module docstring), so a step s leaves 2e-5 / s and
+    s^2 / 6 of the third derivative (each of z's at most 8 along a direction of norm 1 in
+    logits); G's bf16 rounding leaves 2^-8 of the magnitudes."""
+    rows, H, V, t = 64, 64, 300, 1.0
+    g, h, w, y, b, _ = make(rows, H, V)
+    _, lse, ent = pace.token_logprob_entropy(b, h, w, y, t)
+    one = torch.full((rows,), 1.0 / rows, device=DEV)
+    gh, gw = pace.token_logprob_entropy_backward(b, h, w, y, lse, one, ent, 0.3 * one, t,
+                                                 grad_dtype=torch.float32)
+    # steps that bf16 holds: every entry moves by whole units in its last place
+    for x, grad in ((h, gh), (w, gw)):
+        up = (x.float() * (1 + 2.0 ** -7)).to(torch.bfloat16)
+        down = (x.float() * (1 - 2.0 ** -7)).to(torch.bfloat16)
+        step = up.double() - down.double()
+
+        def f(v):
+            hh, ww = (v, w) if x is h else (h, v)
+            lp, _, en = pace.token_logprob_entropy(b, hh, ww, y, t)
+            return (lp.double() + 0.3 * en.double()).mean().item()
+        slope = (grad.double() * step).sum().item()
+        mag = (grad.double().abs() * step.abs()).sum().item()
+        # second order cancels in the symmetric difference but for the steps' own asymmetry
+        assert abs((f(up) - f(down)) - slope) <= 2e-5 + 2.0 ** -8 * mag + 2.0 ** -7 * abs(slope) + 1e-4
+
+
+def test_no_rows():
+    _, h, w, y, _, _ = make(4, 64, 300)
+    b = pace.make_batch(torch.zeros(1, dtype=torch.int64, device=DEV), 0)
+    lp, lse, ent = pace.token_logprob_entropy(b, h[:0], w, y[:0])
+    assert ent.numel() == 0
+    none = torch.empty(0, device=DEV)
+    gw = torch.full((300, 64), math.nan, device=DEV, dtype=torch.bfloat16)
+    pace.token_logprob_entropy_backward(b, h[:0], w, y[:0], none, none, none, none, grad_w=gw)
+    assert (gw == 0).all()
+
+
+def test_other_stream_and_graph():
+    _, h, w, y, b, _ = make(200, 64, 3001, 0.8)
+    want = pace.token_logprob_entropy(b, h, w, y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = pace.token_logprob_entropy(b, h, w, y)
+    side.synchronize()
+    for a, c in zip(want, got):
+        assert torch.equal(a, c)
+    out = [torch.empty(200, device=DEV) for _ in range(3)]
+    ws = pace.workspace(pace.token_logprob_entropy_workspace_size(200, 1, 64, 3001), DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pace.token_logprob_entropy(b, h, w, y, 1.0, None, *out, ws=ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, c in zip(want, out):
+        assert torch.equal(a, c)
+
+
+def test_refusals():
+    _, h, w, y, b, _ = make(4, 64, 300)
+    x = torch.zeros(4, device=DEV)
+    with pytest.raises(ValueError, match="at least 4"):
+        pace.token_logprob_entropy(b, h, w, y, entropy=torch.zeros(3, device=DEV))
+    with pytest.raises(pace.PaceError) as err:  # too small a workspace
+        pace.token_logprob_entropy(b, h, w, y, ws=pace.workspace(1024, DEV))
+    assert err.value.status == pace.ERR_WORKSPACE
+    with pytest.raises(pace.PaceError) as err:  # an entropy gradient without entropies
+        pace.token_logprob_entropy_backward(b, h, w, y, x, x, dentropy=x)
+    assert err.value.status == pace.ERR_INVALID_ARG
+    with pytest.raises(ValueError, match="float16"):
+        pace.token_logprob_entropy_backward(b, h, w, y, x, x,
+                                            grad_w=torch.zeros(300, 64, device=DEV).half())
+    with pytest.raises(ValueError, match="bfloat16"):  # the two gradients are of one type
+        pace.token_logprob_entropy_backward(
+            b, h, w, y, x, x, grad_hidden=torch.zeros(4, 64, device=DEV, dtype=torch.bfloat16),
+            grad_w=torch.zeros(300, 64, device=DEV))
+    L, fake = pace.lib(), 0x1000
+    batch = pace.PaceBatch(fake, None, None, 1, 4)
+    st = L.pace_token_logprob_entropy(ctypes.byref(batch), fake, fake, fake, 64, 300, 1.0, fake,
+                                      fake, None, None, fake, 1 << 30, None, None)
+    assert st == pace.ERR_INVALID_ARG
+    st = L.pace_token_logprob_entropy_backward(ctypes.byref(batch), fake, fake, fake, 64, 300, 1.0,
+                                               fake, fake, fake, fake, pace._DTYPES[torch.float16],
+                                               fake, fake, fake, 1 << 30, None, None)
+    assert st == pace.ERR_INVALID_ARG
