@@ -647,6 +647,67 @@ PACE_API pace_status pace_logits_logprob_backward(const PaceLogits* logits,
                                                   int32_t* status_dev, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Orthogonalised updates                                                    */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+  float lr;           /* default 0.02 */
+  float momentum;     /* mu; default 0.95 */
+  float weight_decay; /* decoupled: the weights shrink by lr * weight_decay; default 0 */
+  float scale;        /* factor of the update beside lr, for example
+                         0.2 sqrt(max(rows, cols)); default 1 */
+  float eps;          /* added to the norm, >= 1e-30; default 1e-7 */
+  float coef[3];      /* a, b, c of the step; default 3.4445, -4.7750, 2.0315 */
+  int32_t nesterov;   /* default 1 */
+  int32_t steps;      /* 1..32; default 5 */
+} PaceMuonParams;
+
+PACE_API void pace_muon_params_default(PaceMuonParams* p);
+
+/* Orthogonalises each matrix of a stack by Newton-Schulz products, as the Muon
+ * optimiser does with its updates:
+ *   X = U / (|U|_F + eps), then `steps` times  A = X X^T,  X <- a X + (b A + c A^2) X
+ * (for rows > cols the same on X^T), which maps X's singular values by
+ * a s + b s^3 + c s^5 a step.  Products are of fp16 operands scaled by powers of two,
+ * with float32 sums: the result is about 1.5e-3 of its norm off the exact steps'
+ * on matrices whose singular values lie within 1:100; what lies further below the
+ * largest is known to fp16's 2^-11 of the largest only.
+ *   x          device float32 or bf16 [batch][rows][cols], rows contiguous, strides
+ *              in elements; rows and cols up to 65,536, batch up to 65,535.
+ *   out        device bf16, the same shape with its own strides; it may be x (bf16,
+ *              same strides).
+ * lr, momentum, weight_decay, scale and nesterov are not used.  A zero matrix stays
+ * zero.  A norm that is infinite or NaN reports PACE_ERR_NAN_INPUT (squares are
+ * float32: entries of 1e19 overflow).  Coefficients under which the steps diverge
+ * give PACE_ERR_INVALID_ARG.  Three launches, one of them cooperative: it needs the
+ * GPU's SMs to itself once they are free, and its waits are bounded (2 s, then
+ * PACE_ERR_TIMEOUT). */
+PACE_API pace_status pace_orthogonalize(const void* x, int32_t dtype, int64_t batch,
+                                        int64_t rows, int64_t cols, int64_t row_stride,
+                                        int64_t batch_stride, const PaceMuonParams* params,
+                                        void* out, int64_t out_row_stride,
+                                        int64_t out_batch_stride, void* workspace,
+                                        size_t workspace_bytes, int32_t* status_dev,
+                                        void* stream);
+
+/* One update of a stack of weight matrices, contiguous [batch][rows][cols]:
+ *   momentum <- mu momentum + grad
+ *   U = grad + mu momentum (nesterov) or momentum;  O = pace_orthogonalize(U)
+ *   weight <- (1 - lr weight_decay) weight - lr scale O
+ * with the last line in the last product's epilogue (O is not written).
+ *   weight, momentum  device float32, updated in place.
+ *   weight_bf16       device bf16 or NULL: receives the new weights rounded.
+ *   grad              device float32 or bf16. */
+PACE_API pace_status pace_muon_update(float* weight, void* weight_bf16, const void* grad,
+                                      int32_t grad_dtype, float* momentum, int64_t batch,
+                                      int64_t rows, int64_t cols, const PaceMuonParams* params,
+                                      void* workspace, size_t workspace_bytes,
+                                      int32_t* status_dev, void* stream);
+
+/* Workspace of both: two copies of X and one of A and B in fp16, and partial sums. */
+PACE_API size_t pace_muon_workspace_size(int64_t batch, int64_t rows, int64_t cols);
+
+/* ------------------------------------------------------------------------ */
 /* Profiling                                                                 */
 /* ------------------------------------------------------------------------ */
 

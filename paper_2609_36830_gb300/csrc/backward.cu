@@ -164,33 +164,11 @@ __host__ __device__ inline TailSplit tail_split(int64_t items, int n_clusters, i
   return s;
 }
 
-// 128-byte-swizzled operand tiles.  K-major: rows of 64 K elements (128 B),
-// 8-row groups 1024 B apart; a 16-deep K step is +32 B.  MN-major: 64 MN
-// elements per 128-byte row, one row per k; boxes of 64 (MN) x 64 (K) stacked
-// along MN 8 KB apart (leading byte offset), 8-k groups 1024 B apart (stride
-// byte offset); a 16-deep K step is +2048 B.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, bool mn_major) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
-  d |= static_cast<uint64_t>(mn_major ? (8192u >> 4) : 1u) << 16;
-  d |= static_cast<uint64_t>(1024u >> 4) << 32;
-  d |= static_cast<uint64_t>(1u) << 46;
-  d |= static_cast<uint64_t>(2u) << 61;
-  return d;
-}
-
 // M = 256: the pair's two 128-row tiles.
 __host__ __device__ constexpr uint32_t idesc_bf16(bool a_mn, bool b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) |
          ((b_mn ? 1u : 0u) << 16) | ((static_cast<uint32_t>(GBN) >> 3) << 17) |
          ((static_cast<uint32_t>(2 * GBM) >> 4) << 24);
-}
-
-// Two floats as bf16 (round to nearest even), the first in the low half.
-__device__ __forceinline__ uint32_t bf16x2_rn(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
 }
 
 template <bool A_MN, bool B_MN, int EPI>

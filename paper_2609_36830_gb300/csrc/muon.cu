@@ -1,0 +1,957 @@
+// Orthogonalised updates by Newton-Schulz products, and the weight update that uses them.
+//
+// With U a matrix (a gradient, or momentum and gradient), X = U / (|U|_F + eps) and the
+// coefficients (a, b, c),
+//   A = X X^T,  B = b A + c A^2,  X <- a X + B X          `steps` times,
+// which drives every singular value of X towards 1 (an odd polynomial of X in its
+// singular values).  For a tall U the same with X^T X and X B, so A and B are s x s, s the
+// shorter side, and X is never transposed: the tensor cores read either operand K-major or
+// MN-major.
+//
+// Types.  The operands are fp16 with a power of two beside each (X, A and B are bounded, see
+// choose_scales), so they keep 11 significant bits where bf16 has 8: on Gaussian matrices
+// the update is 1.1-1.6e-3 off 64 bits where bf16 products are off 9-13e-3; both run at
+// the same rate.  Sums are fp32, in tensor memory.
+//
+// newton_schulz_kernel: one cooperative launch does all the products, 3 `steps` phases with
+// a grid barrier between them (a launch for each would add its start and drain to
+// products of 10-100 us).  In a phase the work items are 256 x 256 tiles, dealt to CTA
+// pairs; per pair the structure of the other tensor-core kernels: warp 0 of each CTA issues
+// TMA loads of its 128 A rows and its half of the B tile into a 4-stage ring, warp 1 of the
+// even CTA issues tcgen05.mma.cta_group::2 (M 256, N 256, K 16), warps 2-5 of each CTA
+// drain one of two accumulators while the next tile is computed.  A and B are symmetric, so
+// only tiles on and below the diagonal are computed and each is also stored
+// transposed: 3 s^2 l + s^3 operations a step instead of 4 s^2 l + 2 s^3.
+// The last phase's epilogue holds the update itself: it is written out in bf16, or goes
+// straight into the weights.
+#include <cuda.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <mutex>
+
+#include "pace_internal.cuh"
+#include "pace_tma.cuh"
+
+#include <cuda_bf16.h>
+
+namespace pace {
+namespace {
+
+constexpr int TM = 256;  // rows and columns of a pair's tile
+constexpr int BM = 128;  // rows of it per CTA
+constexpr int BK = 64;
+constexpr int STAGES = 4;
+constexpr int kThreads = 192;
+constexpr uint32_t kStageA = BM * BK * 2;      // 16 KB
+constexpr uint32_t kStageB = TM / 2 * BK * 2;  // 16 KB: this CTA's half of the B tile
+constexpr uint32_t kStageBytes = kStageA + kStageB;
+constexpr uint32_t kTmemCols = 2 * TM;
+constexpr uint32_t kOutTile = 32 * 128;        // an epilogue warp's staging tile
+constexpr uint32_t kOutBytes = 4 * 2 * kOutTile;
+constexpr size_t kSmemBytes = 1024 + STAGES * kStageBytes + kOutBytes + 256;
+constexpr int kMaxClusters = 76;
+constexpr int kNormBlocks = 128;  // partial sums of a matrix's norm
+
+// A phase's product and what its epilogue makes of it.
+enum { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };
+
+struct Maps {
+  CUtensorMap xk[2], xm[2], ak, bk;     // loads: K-major (64 x 128 boxes), MN-major (64 x 64)
+  CUtensorMap xs[2], as, bs, at, bt;    // stores: 32-row tiles, and transposed ones
+};
+
+struct NsArgs {
+  int64_t s, l;            // shorter and longer side
+  int batch, steps;
+  int tall;                // U has l rows and s columns
+  int64_t ldx, lda;        // row pitch of X, and of A and B
+  int64_t x_rows;          // rows of X
+  __half* x[2];
+  __half *a, *b;
+  float ca, cb, cc;        // the coefficients
+  float sx, sa, sb;        // powers of two: X, A and B are held times these
+  unsigned* ctr;           // arrivals at the grid barriers, zero at launch
+  int32_t* status;
+  // the result: bf16 with strides, or the weights
+  __nv_bfloat16* out;
+  int64_t out_ld, out_bs;
+  float* weight;           // [batch][rows][columns], or null
+  __nv_bfloat16* weight16;
+  float keep, rate;        // weight = keep * weight - rate * O
+  int vec;                 // the result's rows allow 4 columns at a time
+};
+
+__device__ __forceinline__ unsigned ld_acquire(const unsigned* p) {
+  unsigned v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ void red_release(unsigned* p) {
+  asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p) : "memory");
+}
+
+// Orders writes through the generic proxy with the TMA's accesses, both ways.
+__device__ __forceinline__ void fence_proxy_async() {
+  asm volatile("fence.proxy.async;" ::: "memory");
+}
+
+// Waits until `target` epilogue warps have arrived; false after kWaitLimitNs or an abort.
+__device__ __forceinline__ bool wait_phase(const unsigned* ctr, unsigned target,
+                                           volatile int* abort) {
+  if (ld_acquire(ctr) >= target) return true;
+  const uint64_t t0 = global_timer_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (ld_acquire(ctr) >= target) return true;
+    if ((it & 63u) == 0) {
+      if (*abort) return false;
+      if (global_timer_ns() - t0 > kWaitLimitNs) return false;
+    }
+  }
+}
+
+// Item t of a phase: its matrix and the tile's row and column.
+struct Item {
+  int z, i, j;
+};
+
+struct Phase {
+  int kind, cur;           // cur: which X is read
+  bool sym;
+  int ti, tj, per;         // tiles of rows and columns, items of a matrix
+  int64_t n_items;
+  int nkb;                 // K steps
+  const CUtensorMap *ma, *mb;
+  bool a_mn, b_mn;
+
+  __device__ Phase(const NsArgs& p, const Maps& m, int ph) {
+    const int r = ph % 3, step = ph / 3;
+    kind = r == 2 && step == p.steps - 1 ? kLast : r;
+    cur = step & 1;
+    const int ts = static_cast<int>((p.s + TM - 1) / TM), tl = static_cast<int>((p.l + TM - 1) / TM);
+    sym = r != 2;
+    ti = sym || !p.tall ? ts : tl;
+    tj = sym || p.tall ? ts : tl;
+    per = sym ? ts * (ts + 1) / 2 : ti * tj;
+    n_items = static_cast<int64_t>(per) * p.batch;
+    nkb = static_cast<int>(((r == 0 ? p.l : p.s) + BK - 1) / BK);
+    a_mn = b_mn = false;
+    if (r == 0) {
+      ma = mb = p.tall ? &m.xm[cur] : &m.xk[cur];
+      a_mn = b_mn = p.tall;
+    } else if (r == 1) {
+      ma = mb = &m.ak;
+    } else if (p.tall) {
+      ma = &m.xk[cur];
+      mb = &m.bk;
+    } else {
+      ma = &m.bk;
+      mb = &m.xm[cur];
+      b_mn = true;
+    }
+  }
+
+  __device__ Item item(int64_t t) const {
+    Item it;
+    it.z = static_cast<int>(t / per);
+    const int r = static_cast<int>(t - static_cast<int64_t>(it.z) * per);
+    if (sym) {  // row by row of the lower triangle
+      int i = static_cast<int>((sqrtf(8.0f * r + 1.0f) - 1.0f) * 0.5f);
+      while ((i + 1) * (i + 2) / 2 <= r) ++i;
+      while (i * (i + 1) / 2 > r) --i;
+      it.i = i;
+      it.j = r - i * (i + 1) / 2;
+    } else {  // the shorter side's tiles fastest: a round reads all of B and part of X
+      const bool rows_fast = ti <= tj;
+      it.i = rows_fast ? r % ti : r / tj;
+      it.j = rows_fast ? r / ti : r % tj;
+    }
+    return it;
+  }
+};
+
+// fp16 operands, fp32 sums, M 256, N 256.
+__device__ __forceinline__ uint32_t idesc_f16(bool a_mn, bool b_mn) {
+  return (1u << 4) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+         ((static_cast<uint32_t>(TM) >> 3) << 17) | ((static_cast<uint32_t>(TM) >> 4) << 24);
+}
+
+__device__ __forceinline__ uint32_t half2_rn(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// 32 fp16 values of a row (64 bytes, aligned) as floats.
+__device__ __forceinline__ void load_row32(const __half* src, float (&f)[32]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint4 u = __ldcg(reinterpret_cast<const uint4*>(src) + q);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      f[8 * q + 2 * i] = p.x;
+      f[8 * q + 2 * i + 1] = p.y;
+    }
+  }
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    newton_schulz_kernel(const __grid_constant__ Maps maps, const NsArgs p) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * kStageBytes + kOutBytes);
+  uint64_t* full = bars;
+  uint64_t* empty = bars + STAGES;
+  uint64_t* tmem_full = bars + 2 * STAGES;
+  uint64_t* tmem_empty = tmem_full + 2;
+  uint64_t* mma_done = tmem_empty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t crank = cluster_ctarank();
+  const bool leader = crank == 0;
+  const int64_t cid = blockIdx.x / 2, n_clusters = gridDim.x / 2;
+  const int n_phases = 3 * p.steps;
+  const unsigned arrivals = gridDim.x * 4;  // epilogue warps of a phase
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tmem_full[b], 1);
+      mbar_init(&tmem_empty[b], 2 * 4);  // one arrival per epilogue warp of the pair
+    }
+    mbar_init(mma_done, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  cluster_sync();  // both CTAs run and their barriers exist
+  if (warp == 1) {
+    tmem_alloc_pair(tmem_slot, kTmemCols);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  cluster_sync();  // both CTAs' tensor memory is allocated before any MMA writes it
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t peer_abort = cluster_addr(const_cast<int*>(abort_flag), crank ^ 1u);
+  auto give_up = [&]() {
+    if (!*abort_flag) report(p.status, PACE_ERR_TIMEOUT);
+    *abort_flag = 1;
+    st_cluster_u32(peer_abort, 1u);
+  };
+
+  if (warp == 0) {
+    uint64_t pol;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+    uint32_t it = 0;
+    bool ok = true;
+    for (int ph = 0; ph < n_phases && ok; ++ph) {
+      const Phase f(p, maps, ph);
+      if (ph > 0) {  // what this phase reads is written
+        const bool go = lane != 0 || wait_phase(p.ctr, ph * arrivals, abort_flag);
+        if (!__all_sync(0xffffffffu, go)) {
+          ok = false;
+          break;
+        }
+        fence_proxy_async();
+      }
+      const int boxes_a = f.a_mn ? 2 : 1, boxes = boxes_a + (f.b_mn ? 2 : 1);
+      const bool is_a = lane < boxes_a;
+      const int half = is_a ? lane : lane - boxes_a;  // which 64-wide box of an MN-major tile
+      const CUtensorMap* desc = is_a ? f.ma : f.mb;
+      const bool mn = is_a ? f.a_mn : f.b_mn;
+      const uint32_t dst = (is_a ? 0u : kStageA) + half * 8192u;
+      for (int64_t t = cid; t < f.n_items && ok; t += n_clusters) {
+        const Item im = f.item(t);
+        const int32_t r0 = (is_a ? im.i * TM : im.j * TM) + static_cast<int32_t>(crank) * BM;
+        const int32_t x = mn ? r0 + 64 * half : 0, dx = mn ? 0 : BK;
+        const int32_t y = mn ? 0 : r0, dy = mn ? BK : 0;
+        for (int kb = 0; kb < f.nkb; ++kb, ++it) {
+          const uint32_t s = it % STAGES, par = (it / STAGES) & 1u;
+          if (!__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], par ^ 1u, abort_flag))) {
+            ok = false;
+            break;
+          }
+          const uint32_t bar = cluster_addr(&full[s], 0);
+          if (leader && lane == 0) mbar_arrive_expect_tx(&full[s], 2 * kStageBytes);
+          __syncwarp();  // the lanes' loads are one TMA instruction
+          if (lane < boxes)
+            tma_load_3d_pair(smem + s * kStageBytes + dst, desc, bar, x + kb * dx, y + kb * dy,
+                             im.z, pol);
+        }
+      }
+    }
+    if (lane == 0) {
+      if (!ok) give_up();
+      // every copy issued has landed before the CTA exits
+      const uint64_t lim = *abort_flag ? 1000000ull : kWaitLimitNs;
+      for (uint32_t s = 0; s < STAGES && s < it; ++s) {
+        const uint32_t last = it - 1 - ((it - 1 - s) % STAGES);
+        if (leader)
+          mbar_wait_bounded(&full[s], (last / STAGES) & 1u, nullptr, lim);
+        else
+          mbar_wait_bounded(&empty[s], (last / STAGES) & 1u, nullptr, lim);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && leader) {
+      uint32_t it = 0, tc = 0;
+      bool ok = true;
+      for (int ph = 0; ph < n_phases && ok; ++ph) {
+        const Phase f(p, maps, ph);
+        const uint32_t idesc = idesc_f16(f.a_mn, f.b_mn);
+        const uint32_t da = f.a_mn ? 2048 : 32, db = f.b_mn ? 2048 : 32;
+        for (int64_t t = cid; t < f.n_items && ok; t += n_clusters, ++tc) {
+          const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
+          if (!mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u, abort_flag)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t d_tmem = tmem_base + acc * TM;
+          for (int kb = 0; kb < f.nkb; ++kb, ++it) {
+            const uint32_t s = it % STAGES, par = (it / STAGES) & 1u;
+            if (!mbar_wait_bounded(&full[s], par, abort_flag)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t sa = smem_u32(smem + s * kStageBytes);
+            const uint32_t sb = sa + kStageA;
+#pragma unroll
+            for (int k = 0; k < BK / 16; ++k)
+              tc_mma_f16_pair(d_tmem, operand_desc(sa + k * da, f.a_mn),
+                              operand_desc(sb + k * db, f.b_mn), idesc,
+                              (kb > 0 || k > 0) ? 1u : 0u);
+            tc_commit_pair(cluster_addr(&empty[s], 0));
+            tc_commit_pair(cluster_addr(&empty[s], 1));
+          }
+          if (!ok) break;
+          tc_commit_pair(cluster_addr(&tmem_full[acc], 0));
+          tc_commit_pair(cluster_addr(&tmem_full[acc], 1));
+        }
+      }
+      if (!ok) give_up();
+      tc_commit_pair(cluster_addr(mma_done, 0));
+      mbar_wait_bounded(mma_done, 0, nullptr);
+    }
+  } else {
+    const int quad = warp & 3;
+    const uint32_t empty0 = cluster_addr(&tmem_empty[0], 0);
+    const uint32_t empty1 = cluster_addr(&tmem_empty[1], 0);
+    unsigned char* stage = smem + STAGES * kStageBytes + (warp - 2) * 2 * kOutTile;
+    uint32_t tc = 0;
+    bool ok = true;
+    for (int ph = 0; ph < n_phases && ok; ++ph) {
+      const Phase f(p, maps, ph);
+      if (ph > 0) {  // A and X of earlier phases are read below
+        const bool go = lane != 0 || wait_phase(p.ctr, ph * arrivals, abort_flag);
+        if (!__all_sync(0xffffffffu, go)) {
+          give_up();
+          ok = false;
+          break;
+        }
+      }
+      const int64_t rows = f.sym ? p.s : p.x_rows;
+      const int64_t cols = f.sym || p.tall ? p.s : p.l;
+      const __half* src = f.kind == kPoly ? p.a : p.x[f.cur];
+      const int64_t ld = f.kind == kPoly ? p.lda : p.ldx;
+      const CUtensorMap* store = f.kind == kGram ? &maps.as : f.kind == kPoly ? &maps.bs
+                                                                             : &maps.xs[f.cur ^ 1];
+      const CUtensorMap* mirror = f.kind == kGram ? &maps.at : &maps.bt;
+      // value = f_acc * accumulator + f_src * source
+      float f_acc, f_src = 0.0f;
+      if (f.kind == kGram) {
+        f_acc = p.sa / (p.sx * p.sx);
+      } else if (f.kind == kPoly) {
+        f_acc = p.cc * p.sb / (p.sa * p.sa);
+        f_src = p.cb * p.sb / p.sa;
+      } else {
+        const float unit = f.kind == kLast ? 1.0f / p.sx : 1.0f;
+        f_acc = unit / p.sb;
+        f_src = unit * p.ca;
+      }
+      for (int64_t t = cid; t < f.n_items; t += n_clusters, ++tc) {
+        const Item im = f.item(t);
+        const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
+        const bool got = __all_sync(0xffffffffu,
+                                    mbar_wait_bounded(&tmem_full[acc], acc_ph, abort_flag));
+        if (!got) {
+          give_up();
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const int64_t row_w = static_cast<int64_t>(im.i) * TM + crank * BM + quad * 32;
+        const int64_t row = row_w + lane;
+        const uint32_t tbase = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + acc * TM;
+        const __half* srow = src + (static_cast<int64_t>(im.z) * rows + row) * ld;
+#pragma unroll 1
+        for (int c = 0; c < TM; c += 32) {
+          const int64_t col0 = static_cast<int64_t>(im.j) * TM + c;
+          if (row_w >= rows || col0 >= cols) break;  // the same for the warp; later columns too
+          float v[32];
+          tmem_ld_32x32b_x32(tbase + c, v);
+          float x[32];
+          if (f.kind != kGram) {
+            if (row < rows) {
+              load_row32(srow + col0, x);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] = 0.0f;
+            }
+          }
+          tmem_wait_ld();
+          if (f.kind == kGram) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= f_acc;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], f_acc, x[i] * f_src);
+          }
+          if (f.kind != kLast) {
+            // 32 rows x 64 columns leave as one TMA tile of 128-byte rows (128-byte
+            // swizzle: the lanes' 16-byte stores are conflict-free)
+            if ((c & 32) == 0) {
+              if (lane == 0) bulk_wait_read<0>();
+              __syncwarp();
+            }
+            uint32_t h[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i], v[2 * i + 1]);
+            unsigned char* orow = stage + lane * 128;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int at = (c & 32 ? 4 : 0) + q;
+              *reinterpret_cast<uint4*>(orow + ((at ^ (lane & 7)) << 4)) =
+                  make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+            }
+            if (f.sym && im.i != im.j) {  // and transposed: 64 rows of 32
+              uint16_t* tcol =
+                  reinterpret_cast<uint16_t*>(stage + kOutTile) + (c & 32) * 32 + lane;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                tcol[(2 * i) * 32] = static_cast<uint16_t>(h[i] & 0xffffu);
+                tcol[(2 * i + 1) * 32] = static_cast<uint16_t>(h[i] >> 16);
+              }
+            }
+            if ((c & 32) || col0 + 32 >= cols) {
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                const int32_t cb = static_cast<int32_t>(col0 & ~int64_t{63});
+                tma_store_3d(store, stage, cb, static_cast<int32_t>(row_w), im.z);
+                if (f.sym && im.i != im.j)
+                  tma_store_3d(mirror, stage + kOutTile, static_cast<int32_t>(row_w), cb, im.z);
+                bulk_commit();
+              }
+            }
+          } else {
+            // The update.  Through shared memory, so that the warp's accesses to the
+            // result are whole rows of its 32 x 32 block.
+            __syncwarp();
+            float* tile = reinterpret_cast<float*>(stage);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              *reinterpret_cast<float4*>(tile + lane * 32 + ((q ^ (lane & 7)) << 2)) =
+                  make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+            __syncwarp();
+            const int64_t z_row = static_cast<int64_t>(im.z) * rows + row_w;
+            if (p.vec) {  // 4 columns a lane: columns are a multiple of 4
+              const int q = lane & 7;
+              const int64_t col = col0 + 4 * q;
+#pragma unroll 1
+              for (int r = lane >> 3; r < 32; r += 4) {
+                if (row_w + r >= rows || col >= cols) continue;
+                const float4 o =
+                    *reinterpret_cast<const float4*>(tile + r * 32 + ((q ^ (r & 7)) << 2));
+                if (p.weight) {
+                  const int64_t at = (z_row + r) * cols + col;
+                  float4* w4 = reinterpret_cast<float4*>(p.weight + at);
+                  float4 w = *w4;
+                  w.x = fmaf(w.x, p.keep, -p.rate * o.x);
+                  w.y = fmaf(w.y, p.keep, -p.rate * o.y);
+                  w.z = fmaf(w.z, p.keep, -p.rate * o.z);
+                  w.w = fmaf(w.w, p.keep, -p.rate * o.w);
+                  *w4 = w;
+                  if (p.weight16)
+                    *reinterpret_cast<uint2*>(p.weight16 + at) =
+                        make_uint2(bf16x2_rn(w.x, w.y), bf16x2_rn(w.z, w.w));
+                } else {
+                  *reinterpret_cast<uint2*>(p.out + im.z * p.out_bs + (row_w + r) * p.out_ld +
+                                            col) =
+                      make_uint2(bf16x2_rn(o.x, o.y), bf16x2_rn(o.z, o.w));
+                }
+              }
+            } else {  // a column a lane
+              const int64_t col = col0 + lane;
+#pragma unroll 1
+              for (int r = 0; r < 32 && row_w + r < rows; ++r) {
+                if (col >= cols) continue;
+                const float o = tile[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
+                if (p.weight) {
+                  const int64_t at = (z_row + r) * cols + col;
+                  const float w = fmaf(p.weight[at], p.keep, -p.rate * o);
+                  p.weight[at] = w;
+                  if (p.weight16) p.weight16[at] = __float2bfloat16_rn(w);
+                } else {
+                  p.out[im.z * p.out_bs + (row_w + r) * p.out_ld + col] = __float2bfloat16_rn(o);
+                }
+              }
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+      }
+      // this warp's tiles are in memory: the next phase may read them
+      if (lane == 0) {
+        bulk_wait_all();
+        fence_proxy_async();
+        __threadfence();
+        if (ok) red_release(p.ctr);
+      }
+      __syncwarp();
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  // neither CTA frees its tensor memory or leaves while the pair's MMAs, copies
+  // or arrivals may still reach it
+  cluster_sync();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem_base, kTmemCols);
+  cluster_sync();  // the collective release is complete in both CTAs
+}
+
+// ------------------------------------------------------------- norm and first X
+
+// U: a matrix as it is, or momentum and gradient.
+struct UArgs {
+  const void* g;           // float32 or bf16
+  int is_bf16;
+  int64_t ld, bs;          // its strides
+  int64_t rows, cols;
+  float* momentum;         // [batch][rows][cols], or null
+  float mu;
+  int nesterov;
+  int vec;                 // g's, momentum's and X's rows allow 8 columns at a time
+  double* partial;         // [batch][kNormBlocks]
+  __half* x;               // X, times sx
+  int64_t ldx;
+  float sx, eps;
+  int32_t* status;
+};
+
+__device__ __forceinline__ void load8(const UArgs& p, int64_t at, float (&f)[8]) {
+  if (p.is_bf16) {
+    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.g) + at);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  } else {
+    const float4* s = reinterpret_cast<const float4*>(static_cast<const float*>(p.g) + at);
+    const float4 a = s[0], b = s[1];
+    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w;
+    f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+  }
+}
+
+__device__ __forceinline__ float load1(const UArgs& p, int64_t at) {
+  return p.is_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.g)[at])
+                   : static_cast<const float*>(p.g)[at];
+}
+
+// u = mu m + g, or g + mu m under Nesterov, for the updated momentum m
+__device__ __forceinline__ float direction(const UArgs& p, float g, float m) {
+  return p.nesterov ? fmaf(p.mu, m, g) : m;
+}
+
+constexpr int kElemThreads = 512;
+
+// kNorm: updates the momentum and sums the squares of U.  Otherwise: X from the sums.
+// A block takes every kNormBlocks-th group of 8 columns of its matrix, row by row.
+template <bool kNorm>
+__global__ void __launch_bounds__(kElemThreads) direction_kernel(const UArgs p) {
+  const int z = blockIdx.y;
+  const int64_t groups = (p.cols + 7) / 8, n = p.rows * groups;
+  float scale = 0.0f;
+  __shared__ double s_sum[kElemThreads / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (!kNorm) {
+    double sum = 0.0;
+    if (warp == 0) {
+      for (int i = lane; i < kNormBlocks; i += 32) sum += p.partial[z * kNormBlocks + i];
+#pragma unroll
+      for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      if (lane == 0) s_sum[0] = sum;
+    }
+    __syncthreads();
+    const float norm = static_cast<float>(sqrt(s_sum[0]));
+    scale = p.sx / (norm + p.eps);
+    if (!(norm < INFINITY) && blockIdx.x == 0 && threadIdx.x == 0)
+      report(p.status, PACE_ERR_NAN_INPUT);
+  }
+  float ss = 0.0f;
+  double total = 0.0;
+  int terms = 0;
+  for (int64_t v = static_cast<int64_t>(blockIdx.x) * kElemThreads + threadIdx.x; v < n;
+       v += static_cast<int64_t>(gridDim.x) * kElemThreads) {
+    const int64_t row = v / groups, c = (v - row * groups) * 8;
+    const int64_t at = z * p.bs + row * p.ld + c;
+    const int64_t ma = (z * p.rows + row) * p.cols + c;
+    __half* xo = p.x + (z * p.rows + row) * p.ldx + c;
+    float u[8];
+    if (p.vec) {  // columns are a multiple of 8
+      load8(p, at, u);
+      if (p.momentum) {
+        float4* m4 = reinterpret_cast<float4*>(p.momentum + ma);
+        float4 m[2] = {m4[0], m4[1]};
+        float* mf = reinterpret_cast<float*>(m);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (kNorm) mf[i] = fmaf(p.mu, mf[i], u[i]);
+          u[i] = direction(p, u[i], mf[i]);
+        }
+        if (kNorm) m4[0] = m[0], m4[1] = m[1];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        u[i] = 0.0f;
+        if (c + i >= p.cols) continue;
+        u[i] = load1(p, at + i);
+        if (p.momentum) {
+          float m = p.momentum[ma + i];
+          if (kNorm) p.momentum[ma + i] = m = fmaf(p.mu, m, u[i]);
+          u[i] = direction(p, u[i], m);
+        }
+      }
+    }
+    if (kNorm) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(u[i], u[i], ss);
+      if (++terms == 64) {  // into 64 bits before the float's own rounding tells
+        total += ss;
+        ss = 0.0f;
+        terms = 0;
+      }
+    } else {  // X's rows are padded to whole groups
+      *reinterpret_cast<uint4*>(xo) =
+          make_uint4(half2_rn(u[0] * scale, u[1] * scale), half2_rn(u[2] * scale, u[3] * scale),
+                     half2_rn(u[4] * scale, u[5] * scale), half2_rn(u[6] * scale, u[7] * scale));
+    }
+  }
+  if (kNorm) {
+    total += ss;
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) total += __shfl_xor_sync(0xffffffffu, total, x);
+    if (lane == 0) s_sum[warp] = total;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      double sum = 0.0;
+      for (int w = 0; w < kElemThreads / 32; ++w) sum += s_sum[w];
+      p.partial[z * kNormBlocks + blockIdx.x] = sum;
+    }
+  }
+}
+
+// ------------------------------------------------------------- host side
+
+struct MuonWs {
+  __half *x[2], *a, *b;
+  double* partial;
+  unsigned* ctr;
+  int64_t ldx, lda;
+};
+
+void carve_muon_ws(Carver& cv, int64_t batch, int64_t rows, int64_t cols, MuonWs* w) {
+  const int64_t s = rows < cols ? rows : cols;
+  w->ldx = static_cast<int64_t>(align_up(static_cast<size_t>(cols), 64));
+  w->lda = static_cast<int64_t>(align_up(static_cast<size_t>(s), 64));
+  const size_t nx = static_cast<size_t>(batch) * rows * w->ldx;
+  const size_t na = static_cast<size_t>(batch) * s * w->lda;
+  for (int i = 0; i < 2; ++i) w->x[i] = cv.take<__half>(nx);
+  w->a = cv.take<__half>(na);
+  w->b = cv.take<__half>(na);
+  w->partial = cv.take<double>(static_cast<size_t>(batch) * kNormBlocks);
+  w->ctr = cv.take<unsigned>(1);
+}
+
+// The largest |a x + b x^3 + c x^5| (odd) or |b x + c x^2| over 0 <= x <= r.
+double largest_step(double a, double b, double c, double r) {
+  auto f = [&](double x) { return fabs(x * (a + x * x * (b + c * x * x))); };
+  double m = f(r);
+  // f' = a + 3 b y + 5 c y^2 with y = x^2
+  const double q2 = 5 * c, q1 = 3 * b, disc = q1 * q1 - 4 * q2 * a;
+  if (q2 != 0 && disc >= 0) {
+    for (int sign = -1; sign <= 1; sign += 2) {
+      const double y = (-q1 + sign * sqrt(disc)) / (2 * q2);
+      if (y > 0 && y < r * r) m = fmax(m, f(sqrt(y)));
+    }
+  } else if (q2 == 0 && q1 != 0 && -a / q1 > 0 && -a / q1 < r * r) {
+    m = fmax(m, f(sqrt(-a / q1)));
+  }
+  return m;
+}
+double largest_poly(double b, double c, double r) {
+  double m = fabs(r * (b + c * r));
+  const double y = c != 0 ? -b / (2 * c) : -1;
+  if (y > 0 && y < r) m = fmax(m, fabs(y * (b + c * y)));
+  return m;
+}
+
+// Powers of two that keep X, A and B inside fp16 and as far up in it as they can be.  X's
+// singular values start at most 1 (its Frobenius norm is) and a step maps them by the odd
+// polynomial, so its largest value R over all steps bounds X's entries, R^2 those of A and
+// the quadratic's largest value over [0, R^2] those of B.  1 % more at every step and 5 %
+// at the end for rounding.
+bool choose_scales(const PaceMuonParams* q, NsArgs* p) {
+  double r = 1.0, most = 1.0;
+  for (int i = 0; i < q->steps; ++i) {
+    r = 1.01 * largest_step(q->coef[0], q->coef[1], q->coef[2], r);
+    most = fmax(most, r);
+    if (!(most <= 16.0)) return false;  // the steps diverge
+  }
+  auto scale = [](double bound) {
+    return static_cast<float>(exp2(floor(log2(60000.0 / fmax(bound, 1e-3)))));
+  };
+  p->sx = scale(1.05 * most);
+  p->sa = scale(1.05 * most * most);
+  p->sb = scale(1.05 * largest_poly(q->coef[1], q->coef[2], 1.05 * most * most));
+  return true;
+}
+
+pace_status ns_max_clusters(int* out) {
+  constexpr int kMaxDevices = 64;
+  static int cached[kMaxDevices];
+  static std::mutex mu;
+  int dev = 0;
+  PACE_TRY_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return PACE_ERR_CUDA;
+  std::lock_guard<std::mutex> g(mu);
+  if (cached[dev] == 0) {
+    PACE_TRY_CUDA(cudaFuncSetAttribute(newton_schulz_kernel,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(kSmemBytes)));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(sm_count()) & ~1u, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    PACE_TRY_CUDA(cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel, &cfg));
+    if (n < 1) return PACE_ERR_CUDA;
+    cached[dev] = n < kMaxClusters ? n : kMaxClusters;
+  }
+  *out = cached[dev];
+  return PACE_OK;
+}
+
+pace_status check_params(const PaceMuonParams* q) {
+  if (!q || q->steps < 1 || q->steps > 32) return PACE_ERR_INVALID_ARG;
+  for (float v : {q->lr, q->momentum, q->weight_decay, q->scale, q->eps, q->coef[0], q->coef[1],
+                  q->coef[2]})
+    if (!isfinite(v)) return PACE_ERR_INVALID_ARG;
+  // eps keeps a zero matrix's quotient finite
+  if (!(q->eps >= 1e-30f)) return PACE_ERR_INVALID_ARG;
+  return PACE_OK;
+}
+
+pace_status check_shape(int32_t dtype, int64_t batch, int64_t rows, int64_t cols) {
+  if (dtype != PACE_F32 && dtype != PACE_BF16) return PACE_ERR_INVALID_ARG;
+  if (batch < 0 || rows < 0 || cols < 0) return PACE_ERR_INVALID_ARG;
+  if (batch > 65535 || rows > 65536 || cols > 65536) return PACE_ERR_UNSUPPORTED_SHAPE;
+  return PACE_OK;
+}
+
+// Norm, X, and the products; u and n hold what differs between the two entry points.
+pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonParams* q,
+                              void* workspace, size_t workspace_bytes, cudaStream_t st) {
+  if (!choose_scales(q, &n)) return PACE_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 256)) return PACE_ERR_WORKSPACE;
+  Carver cv(workspace, workspace_bytes);
+  MuonWs w;
+  carve_muon_ws(cv, batch, u.rows, u.cols, &w);
+  if (!cv.fits()) return PACE_ERR_WORKSPACE;
+  u.partial = w.partial;
+  u.x = w.x[0];
+  u.ldx = w.ldx;
+  u.sx = n.sx;
+  u.eps = q->eps;
+  n.tall = u.rows > u.cols ? 1 : 0;
+  n.s = n.tall ? u.cols : u.rows;
+  n.l = n.tall ? u.rows : u.cols;
+  n.x_rows = u.rows;
+  n.batch = static_cast<int>(batch);
+  n.steps = q->steps;
+  n.ldx = w.ldx;
+  n.lda = w.lda;
+  n.x[0] = w.x[0];
+  n.x[1] = w.x[1];
+  n.a = w.a;
+  n.b = w.b;
+  n.ca = q->coef[0];
+  n.cb = q->coef[1];
+  n.cc = q->coef[2];
+  n.ctr = w.ctr;
+
+  Maps m;
+  const int64_t xbs = u.rows * w.ldx, abs_ = n.s * w.lda;
+  for (int i = 0; i < 2; ++i) {
+    PACE_TRY(encode_f16_3d(&m.xk[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, BM, true));
+    PACE_TRY(encode_f16_3d(&m.xm[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 64, true));
+    PACE_TRY(encode_f16_3d(&m.xs[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 32, true));
+  }
+  PACE_TRY(encode_f16_3d(&m.ak, w.a, batch, n.s, n.s, w.lda, abs_, 64, BM, true));
+  PACE_TRY(encode_f16_3d(&m.bk, w.b, batch, n.s, n.s, w.lda, abs_, 64, BM, true));
+  PACE_TRY(encode_f16_3d(&m.as, w.a, batch, n.s, n.s, w.lda, abs_, 64, 32, true));
+  PACE_TRY(encode_f16_3d(&m.bs, w.b, batch, n.s, n.s, w.lda, abs_, 64, 32, true));
+  PACE_TRY(encode_f16_3d(&m.at, w.a, batch, n.s, n.s, w.lda, abs_, 32, 64, false));
+  PACE_TRY(encode_f16_3d(&m.bt, w.b, batch, n.s, n.s, w.lda, abs_, 32, 64, false));
+
+  int max_clusters = 0;
+  PACE_TRY(ns_max_clusters(&max_clusters));
+  PACE_TRY_CUDA(cudaMemsetAsync(w.ctr, 0, sizeof(unsigned), st));
+  const dim3 egrid(kNormBlocks, static_cast<unsigned>(batch), 1);
+  direction_kernel<true><<<egrid, kElemThreads, 0, st>>>(u);
+  PACE_TRY(last_launch_status());
+  direction_kernel<false><<<egrid, kElemThreads, 0, st>>>(u);
+  PACE_TRY(last_launch_status());
+
+  const int64_t ts = (n.s + TM - 1) / TM, tl = (n.l + TM - 1) / TM;
+  const int64_t items = batch * (ts * tl > ts * (ts + 1) / 2 ? ts * tl : ts * (ts + 1) / 2);
+  const int64_t clusters = items < max_clusters ? items : max_clusters;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(2 * clusters), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;  // every CTA is resident: the barriers' waits end
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, newton_schulz_kernel, m, n) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return PACE_ERR_CUDA;
+  }
+  return last_launch_status();
+}
+
+}  // namespace
+}  // namespace pace
+
+using namespace pace;
+
+extern "C" void pace_muon_params_default(PaceMuonParams* p) {
+  if (!p) return;
+  p->lr = 2e-2f;
+  p->momentum = 0.95f;
+  p->weight_decay = 0.0f;
+  p->scale = 1.0f;
+  p->eps = 1e-7f;
+  p->coef[0] = 3.4445f;
+  p->coef[1] = -4.7750f;
+  p->coef[2] = 2.0315f;
+  p->nesterov = 1;
+  p->steps = 5;
+}
+
+extern "C" size_t pace_muon_workspace_size(int64_t batch, int64_t rows, int64_t cols) {
+  if (batch < 0 || rows < 0 || cols < 0) return 0;
+  Carver cv;
+  MuonWs w;
+  carve_muon_ws(cv, batch, rows, cols, &w);
+  return cv.used;
+}
+
+extern "C" pace_status pace_orthogonalize(const void* x, int32_t dtype, int64_t batch,
+                                          int64_t rows, int64_t cols, int64_t row_stride,
+                                          int64_t batch_stride, const PaceMuonParams* params,
+                                          void* out, int64_t out_row_stride,
+                                          int64_t out_batch_stride, void* workspace,
+                                          size_t workspace_bytes, int32_t* status_dev,
+                                          void* stream) {
+  PACE_TRY(check_shape(dtype, batch, rows, cols));
+  PACE_TRY(check_params(params));
+  if (batch == 0 || rows == 0 || cols == 0) return PACE_OK;
+  if (!x || !out || row_stride < cols || out_row_stride < cols) return PACE_ERR_INVALID_ARG;
+  if (batch > 1 && (batch_stride < 0 || out_batch_stride < (rows - 1) * out_row_stride + cols))
+    return PACE_ERR_INVALID_ARG;
+  const size_t elem = dtype == PACE_BF16 ? 2 : 4;
+  if (!aligned(x, elem) || !aligned(out, 2)) return PACE_ERR_UNSUPPORTED_SHAPE;
+  UArgs u = {};
+  u.g = x;
+  u.is_bf16 = dtype == PACE_BF16;
+  u.ld = row_stride;
+  u.bs = batch > 1 ? batch_stride : 0;
+  u.rows = rows;
+  u.cols = cols;
+  const int64_t e16 = static_cast<int64_t>(16 / elem);
+  u.vec = cols % 8 == 0 && aligned(x, 16) && u.ld % e16 == 0 && u.bs % e16 == 0;
+  u.status = status_dev;
+  NsArgs n = {};
+  n.out = static_cast<__nv_bfloat16*>(out);
+  n.out_ld = out_row_stride;
+  n.out_bs = batch > 1 ? out_batch_stride : 0;
+  n.vec = cols % 4 == 0 && aligned(out, 8) && n.out_ld % 4 == 0 && n.out_bs % 4 == 0;
+  n.status = status_dev;
+  return run_newton_schulz(u, n, batch, params, workspace, workspace_bytes, as_stream(stream));
+}
+
+extern "C" pace_status pace_muon_update(float* weight, void* weight_bf16, const void* grad,
+                                        int32_t grad_dtype, float* momentum, int64_t batch,
+                                        int64_t rows, int64_t cols, const PaceMuonParams* params,
+                                        void* workspace, size_t workspace_bytes,
+                                        int32_t* status_dev, void* stream) {
+  PACE_TRY(check_shape(grad_dtype, batch, rows, cols));
+  PACE_TRY(check_params(params));
+  if (batch == 0 || rows == 0 || cols == 0) return PACE_OK;
+  if (!weight || !grad || !momentum) return PACE_ERR_INVALID_ARG;
+  const size_t elem = grad_dtype == PACE_BF16 ? 2 : 4;
+  if (!aligned(weight, 4) || !aligned(weight_bf16, 2) || !aligned(grad, elem) ||
+      !aligned(momentum, 4))
+    return PACE_ERR_UNSUPPORTED_SHAPE;
+  UArgs u = {};
+  u.g = grad;
+  u.is_bf16 = grad_dtype == PACE_BF16;
+  u.ld = cols;
+  u.bs = rows * cols;
+  u.rows = rows;
+  u.cols = cols;
+  u.momentum = momentum;
+  u.mu = params->momentum;
+  u.nesterov = params->nesterov;
+  u.vec = cols % 8 == 0 && aligned(grad, 16) && aligned(momentum, 16);
+  u.status = status_dev;
+  NsArgs n = {};
+  n.weight = weight;
+  n.weight16 = static_cast<__nv_bfloat16*>(weight_bf16);
+  n.keep = 1.0f - params->lr * params->weight_decay;
+  n.rate = params->lr * params->scale;
+  n.vec = cols % 4 == 0 && aligned(weight, 16) && aligned(weight_bf16, 8);
+  n.status = status_dev;
+  return run_newton_schulz(u, n, batch, params, workspace, workspace_bytes, as_stream(stream));
+}

@@ -254,6 +254,18 @@ __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const void* des
       : "memory");
 }
 
+// The same for one box of a 3-D tensor map (column x, row y, matrix z).
+__device__ __forceinline__ void tma_load_3d_pair(void* smem_dst, const void* desc,
+                                                 uint32_t bar_caddr, int32_t x, int32_t y,
+                                                 int32_t z, uint64_t cache_hint) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      ".L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;" ::"r"(smem_u32(smem_dst)),
+      "l"(reinterpret_cast<uint64_t>(desc)), "r"(bar_caddr), "r"(x), "r"(y), "r"(z),
+      "l"(cache_hint)
+      : "memory");
+}
+
 // Four whole rows (r0..r3) of a 2-D tensor map whose box is one row high,
 // starting at column x, into this CTA's shared memory at smem_dst, one row
 // after the other; the transaction bytes (4 box rows) complete on the mbarrier
@@ -284,6 +296,15 @@ __device__ __forceinline__ void tma_store_2d(const void* desc, const void* smem_
                    reinterpret_cast<uint64_t>(desc)),
                "r"(smem_u32(smem_src)), "r"(x), "r"(y)
                : "memory");
+}
+
+__device__ __forceinline__ void tma_store_3d(const void* desc, const void* smem_src, int32_t x,
+                                             int32_t y, int32_t z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+          reinterpret_cast<uint64_t>(desc)),
+      "r"(smem_u32(smem_src)), "r"(x), "r"(y), "r"(z)
+      : "memory");
 }
 
 // This thread's stores so far form a group; waits until at most N groups have yet to
@@ -406,6 +427,28 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(uint32_t m, uint32_t n) {
          | (1u << 10)         // B format: bf16
          | ((n >> 3) << 17)   // N / 8
          | ((m >> 4) << 24);  // M / 16
+}
+
+// 128-byte-swizzled operand tiles.  K-major: rows of 64 K elements (128 B),
+// 8-row groups 1024 B apart; a 16-deep K step is +32 B.  MN-major: 64 MN
+// elements per 128-byte row, one row per k; boxes of 64 (MN) x 64 (K) stacked
+// along MN 8 KB apart (leading byte offset), 8-k groups 1024 B apart (stride
+// byte offset); a 16-deep K step is +2048 B.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, bool mn_major) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(mn_major ? (8192u >> 4) : 1u) << 16;
+  d |= static_cast<uint64_t>(1024u >> 4) << 32;
+  d |= static_cast<uint64_t>(1u) << 46;
+  d |= static_cast<uint64_t>(2u) << 61;
+  return d;
+}
+
+// Two floats as bf16 (round to nearest even), the first in the low half.
+__device__ __forceinline__ uint32_t bf16x2_rn(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
 }
 
 __device__ __forceinline__ float ex2_approx(float x) {

@@ -68,6 +68,11 @@ class PaceLogits(ctypes.Structure):
                 ("row_stride", _I64), ("allowed", _P), ("allowed_stride", _I64), ("mask", _P)]
 
 
+class PaceMuonParams(ctypes.Structure):
+    _fields_ = [("lr", _F32), ("momentum", _F32), ("weight_decay", _F32), ("scale", _F32),
+                ("eps", _F32), ("coef", _F32 * 3), ("nesterov", _I32), ("steps", _I32)]
+
+
 # every symbol include/pace.h declares, with its C signature
 SIGNATURES = {
     "pace_status_string": ([_I32], ctypes.c_char_p),
@@ -115,6 +120,11 @@ SIGNATURES = {
     "pace_token_logprob_entropy_backward_workspace_size": ([_I64, _I64, _I32, _I32, _I32], _SZ),
     "pace_logits_logprob": ([_P, _P, _F32, _I32, _P, _P, _P, _P, _P, _P, _P, _P], _I32),
     "pace_logits_logprob_backward": ([_P, _P, _F32, _P, _P, _P, _P, _P, _I64, _P, _P], _I32),
+    "pace_muon_params_default": ([_P], None),
+    "pace_orthogonalize": ([_P, _I32, _I64, _I64, _I64, _I64, _I64, _P, _P, _I64, _I64, _P, _SZ,
+                            _P, _P], _I32),
+    "pace_muon_update": ([_P, _P, _P, _I32, _P, _I64, _I64, _I64, _P, _P, _SZ, _P, _P], _I32),
+    "pace_muon_workspace_size": ([_I64, _I64, _I64], _SZ),
     "pace_set_profile_events": ([_I32, _P, _P], _I32),
     "pace_set_lmhead_splits": ([_I32], _I32),
     "pace_set_score_fused_min_traj": ([_I64], _I32),
@@ -798,3 +808,84 @@ def logits_logprob_backward(lg: PaceLogits, targets, stats, dlp, entropy=None, d
         _arg(status, _I32T, 1, "status"), _stream(stream))
     _check(st, "pace_logits_logprob_backward")
     return grad
+
+
+# ---------------------------------------------------------------- orthogonalised updates
+
+def muon_params(lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True, scale=1.0, steps=5,
+                coef=(3.4445, -4.7750, 2.0315), eps=1e-7):
+    return PaceMuonParams(float(lr), float(momentum), float(weight_decay), float(scale),
+                          float(eps), (_F32 * 3)(*coef), int(bool(nesterov)), int(steps))
+
+
+def muon_workspace_size(batch, rows, cols):
+    return lib().pace_muon_workspace_size(int(batch), int(rows), int(cols))
+
+
+def _stack_arg(t, dtypes, shape, name: str):
+    """(device pointer, row stride, batch stride) of a stack [batch, rows, cols] of
+    matrices with contiguous rows, or of one matrix [rows, cols]."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if not t.is_cuda or t.get_device() != _current_device():
+        raise ValueError(f"{name}: expected a tensor on the current CUDA device")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: expected {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if t.dim() not in (2, 3) or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: expected shape {shape or '[batch, rows, columns]'}, got "
+                         f"{tuple(t.shape)}")
+    rows, cols = t.shape[-2:]
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: expected contiguous rows")
+    ld = t.stride(-2) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{name}: rows overlap (stride {ld}, {cols} columns)")
+    return t.data_ptr(), ld, (t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else rows * ld)
+
+
+def _stack_shape(t):
+    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
+
+
+def orthogonalize(x, params=None, out=None, ws=None, status=None, stream=None):
+    """pace_orthogonalize: bf16, of x's shape.  x: float32 or bf16 [rows, cols] or
+    [batch, rows, cols] with contiguous rows."""
+    ptr, ld, bs = _stack_arg(x, (_F32T, _BF16), None, "x")
+    b, m, n = _stack_shape(x)
+    if out is None:
+        out = torch.empty(x.shape, dtype=_BF16, device=x.device)
+    optr, old, obs = _stack_arg(out, (_BF16,), x.shape, "out")
+    if ws is None:
+        ws = workspace(muon_workspace_size(b, m, n), x.device)
+    p = params or muon_params()
+    st = lib().pace_orthogonalize(ptr, _DTYPES[x.dtype], b, m, n, ld, bs, ctypes.byref(p), optr,
+                                  old, obs, _arg(ws, _U8, None, "ws"), ws.numel(),
+                                  _arg(status, _I32T, 1, "status"), _stream(stream))
+    _check(st, "pace_orthogonalize")
+    return out
+
+
+def muon_update(weight, grad, momentum, params=None, weight_bf16=None, ws=None, status=None,
+                stream=None):
+    """pace_muon_update: one update of weight and momentum in place (float32, contiguous,
+    [rows, cols] or [batch, rows, cols]); grad is float32 or bf16, weight_bf16 an optional
+    bf16 copy of the new weights."""
+    if weight.dim() not in (2, 3):
+        raise ValueError(f"weight: expected [batch, rows, columns], got {tuple(weight.shape)}")
+    b, m, n = _stack_shape(weight)
+    for t, name in ((grad, "grad"), (momentum, "momentum"), (weight_bf16, "weight_bf16")):
+        if t is not None and t.shape != weight.shape:
+            raise ValueError(f"{name}: expected shape {tuple(weight.shape)}, got "
+                             f"{tuple(t.shape)}")
+    if grad.dtype not in (_F32T, _BF16):
+        raise ValueError(f"grad: expected float32 or bfloat16, got {grad.dtype}")
+    if ws is None:
+        ws = workspace(muon_workspace_size(b, m, n), weight.device)
+    p = params or muon_params()
+    st = lib().pace_muon_update(
+        _arg(weight, _F32T, None, "weight"), _arg(weight_bf16, _BF16, None, "weight_bf16"),
+        _arg(grad, grad.dtype, None, "grad"), _DTYPES[grad.dtype],
+        _arg(momentum, _F32T, None, "momentum"), b, m, n, ctypes.byref(p),
+        _arg(ws, _U8, None, "ws"), ws.numel(), _arg(status, _I32T, 1, "status"), _stream(stream))
+    _check(st, "pace_muon_update")
+    return weight

@@ -1,0 +1,255 @@
+"""Newton-Schulz orthogonalisation and the weight update against the steps in 64 bits.
+
+Tolerance.  X, A and B are rounded to fp16, 2^-11 of each entry, twice to three times a step;
+on matrices of Gaussian entries (also with some strong directions) the roundings act like
+independent noise of 2^-11 / sqrt(3) of the norm each, and a step multiplies what X carries
+by at most a = 3.4445 where singular values are small and by less than one where they are
+not: over five steps 15 roundings come to about 4e-3 of the result's norm at most (REL).
+Single entries of such noise stay below six times its root mean square (10^7 entries).  The
+bf16 result is rounded once more, 2^-8 of an entry at most."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2609_36830_gb300 import pace
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+REL = 4e-3
+COEF = (3.4445, -4.7750, 2.0315)
+
+
+def steps64(u, steps=5, coef=COEF, eps=1e-7):
+    x = u.double()
+    tall = x.shape[-2] > x.shape[-1]
+    x = x.transpose(-1, -2) if tall else x
+    x = x / (x.square().sum((-1, -2), keepdim=True).sqrt() + eps)
+    for _ in range(steps):
+        a = x @ x.transpose(-1, -2)
+        x = coef[0] * x + (coef[1] * a + coef[2] * (a @ a)) @ x
+    return x.transpose(-1, -2) if tall else x
+
+
+def gauss(*shape, seed=0, strong=0, dtype=torch.float32, scale=1e-3):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed + sum(shape))
+    u = torch.randn(shape, device=DEV, generator=g)
+    if strong:
+        u = u + torch.randn(*shape[:-1], strong, device=DEV, generator=g) @ torch.randn(
+            *shape[:-2], strong, shape[-1], device=DEV, generator=g) / math.sqrt(strong)
+    return (u * scale).to(dtype)
+
+
+def check(got, want, rel=REL):
+    got, want = got.double(), want.double()
+    assert got.shape == want.shape and torch.isfinite(got).all()
+    for g, w in zip(got.reshape(-1, *got.shape[-2:]), want.reshape(-1, *want.shape[-2:])):
+        d = (g - w).abs()
+        noise = torch.linalg.norm(w).item() * rel
+        assert (d.square().sum().sqrt().item()
+                <= noise + 2.0 ** -9 * torch.linalg.norm(w).item()), d.square().sum().sqrt() / w.norm()
+        assert (d <= 6 * noise / math.sqrt(w.numel()) + 2.0 ** -8 * w.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("b,m,n", [
+    (1, 8, 8), (1, 3, 300), (1, 300, 3), (2, 64, 64), (1, 65, 63), (3, 129, 130), (1, 255, 257),
+    (1, 256, 256), (2, 300, 1000), (2, 1000, 300), (1, 513, 512), (1, 700, 3001), (1, 2731, 1023),
+    (5, 400, 400), (1, 2048, 2048)])
+def test_orthogonalize(b, m, n, dtype):
+    u = gauss(b, m, n, strong=max(1, min(m, n) // 16), dtype=dtype)
+    status = pace.new_status(DEV)
+    got = pace.orthogonalize(u, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    check(got, steps64(u))
+
+
+@pytest.mark.parametrize("m,n", [(1, 1), (1, 7), (7, 1), (1, 5000), (5000, 1)])
+def test_vectors(m, n):
+    """One singular value: u / |u| times the steps' map of 1."""
+    u = gauss(m, n, seed=3)
+    check(pace.orthogonalize(u), steps64(u))
+
+
+def test_singular_values_come_near_one():
+    u = gauss(600, 900, seed=5)
+    s = torch.linalg.svdvals(pace.orthogonalize(u).double())
+    assert s.min().item() > 0.3 and s.max().item() < 1.3
+
+
+@pytest.mark.parametrize("scale", [1e-12, 1.0, 1e12])
+def test_scale_of_the_input(scale):
+    """The update does not depend on U's scale while eps is small beside its norm; a norm
+    far below eps gives X below eps' share of it, as the formula says."""
+    u = gauss(200, 300, seed=9, scale=1.0) * scale
+    check(pace.orthogonalize(u, pace.muon_params(eps=1e-20)), steps64(u, eps=1e-20))
+
+
+def test_zero_one_and_identity():
+    z = torch.zeros(2, 300, 200, device=DEV)
+    assert (pace.orthogonalize(z) == 0).all()
+    eye = torch.eye(256, device=DEV)
+    check(pace.orthogonalize(eye), steps64(eye))
+    half = torch.zeros(3, 130, 140, device=DEV)  # one matrix of the stack is zero
+    half[1] = gauss(130, 140)
+    got = pace.orthogonalize(half)
+    assert (got[0] == 0).all() and (got[2] == 0).all()
+    check(got[1], steps64(half[1]))
+
+
+@pytest.mark.parametrize("steps,coef", [(1, COEF), (2, COEF), (3, (1.5, -0.5, 0.0)),
+                                        (12, (1.5, -0.5, 0.0)), (4, (2.0, -1.5, 0.5)),
+                                        (1, (1.0, 0.0, 0.0))])
+@pytest.mark.parametrize("m,n", [(300, 520), (520, 300)])
+def test_steps_and_coefficients(steps, coef, m, n):
+    u = gauss(m, n, seed=2)
+    got = pace.orthogonalize(u, pace.muon_params(steps=steps, coef=coef))
+    # twelve steps round 36 times, each carried on by at most 1.5 per step
+    check(got, steps64(u, steps, coef), REL * (2 if steps > 5 else 1))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad", [1, 4, 8])
+def test_strides(dtype, pad):
+    buf = torch.full((3, 90 + pad, 200 + pad), math.nan, device=DEV, dtype=dtype)
+    u = buf[:, pad:, :200]
+    u.copy_(gauss(3, 90, 200, dtype=dtype))
+    obuf = torch.full((3, 90 + pad, 200 + pad), 7.0, device=DEV, dtype=torch.bfloat16)
+    out = obuf[:, :90, pad:]
+    pace.orthogonalize(u, out=out)
+    check(out, steps64(u))
+    assert (obuf[:, 90:] == 7.0).all() and (obuf[:, :90, :pad] == 7.0).all()
+
+
+def test_in_place():
+    u = gauss(2, 257, 130, dtype=torch.bfloat16)
+    want = pace.orthogonalize(u)
+    assert torch.equal(pace.orthogonalize(u, out=u), want)
+
+
+def test_the_same_bits_again_on_another_stream_and_in_a_graph():
+    u = gauss(2, 700, 520, dtype=torch.bfloat16)
+    want = pace.orthogonalize(u)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = pace.orthogonalize(u)
+    side.synchronize()
+    assert torch.equal(got, want)
+    ws = pace.workspace(pace.muon_workspace_size(2, 700, 520), DEV)
+    out = torch.zeros_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pace.orthogonalize(u, out=out, ws=ws)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_a_workspace_serves_smaller_and_other_shapes():
+    ws = pace.workspace(pace.muon_workspace_size(1, 1000, 1100), DEV)
+    for m, n in ((1000, 1100), (33, 900), (900, 33), (512, 512)):
+        u = gauss(m, n)
+        check(pace.orthogonalize(u, ws=ws), steps64(u))
+
+
+def test_nan_is_reported():
+    for bad in (math.nan, math.inf):
+        u = gauss(2, 100, 130)
+        u[1, 50, 60] = bad
+        status = pace.new_status(DEV)
+        got = pace.orthogonalize(u, status=status)
+        torch.cuda.synchronize()
+        assert int(status.item()) == pace.ERR_NAN_INPUT
+        check(got[0], steps64(u[0]))  # the other matrix is not touched by it
+
+
+# ---------------------------------------------------------------- the weight update
+
+@pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("shape", [(64, 96), (3, 130, 257), (511, 300), (2, 512, 1024)])
+def test_muon_update(shape, nesterov, gdtype):
+    q = dict(lr=0.02, momentum=0.9, weight_decay=0.1, scale=0.7, nesterov=nesterov)
+    w, m = gauss(*shape, seed=1, scale=0.05), gauss(*shape, seed=2, scale=2e-3)
+    w64, m64 = w.double(), m.double()
+    copy = torch.empty(shape, dtype=torch.bfloat16, device=DEV)
+    for i in range(3):
+        g = gauss(*shape, seed=10 + i, dtype=gdtype)
+        before = w.double()
+        m64 = 0.9 * m64 + g.double()
+        o = steps64(g.double() + 0.9 * m64 if nesterov else m64)
+        status = pace.new_status(DEV)
+        pace.muon_update(w, g, m, pace.muon_params(**q), weight_bf16=copy, status=status)
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        # two roundings of each momentum a step, of mu and of the sum
+        assert ((m.double() - m64).abs() <= 4 * (i + 1) * 2.0 ** -24 * (m64.abs() + g.double().abs())
+                + 1e-9).all()
+        w64 = before * (1 - 0.02 * 0.1) - 0.02 * 0.7 * o
+        noise = 0.02 * 0.7 * REL * torch.linalg.norm(o, dim=(-2, -1), keepdim=True) / math.sqrt(
+            shape[-1] * shape[-2])
+        assert ((w.double() - w64).abs() <= 6 * noise + 2.0 ** -22 * w64.abs()).all()
+        assert torch.equal(copy, w.to(torch.bfloat16))
+
+
+def test_update_of_unaligned_tensors():
+    base = [torch.zeros(100 * 104 + 1, device=DEV) for _ in range(3)]
+    w, g, m = (t[1:].view(100, 104) for t in base)
+    w.copy_(gauss(100, 104, seed=1))
+    g.copy_(gauss(100, 104, seed=2))
+    w2, m2 = w.clone(), m.clone()
+    pace.muon_update(w, g, m)
+    pace.muon_update(w2, g.clone(), m2)
+    assert torch.equal(w, w2) and torch.equal(m, m2)
+
+
+def test_nothing_to_do():
+    for shape in ((0, 5), (5, 0), (0, 3, 3)):
+        u = torch.zeros(shape, device=DEV)
+        assert pace.orthogonalize(u).shape == u.shape
+        pace.muon_update(u, u, u.clone())
+
+
+def test_refusals():
+    u = gauss(16, 32)
+    for kw in (dict(steps=0), dict(steps=33), dict(eps=0.0), dict(coef=(9.0, 0.0, 0.0)),
+               dict(coef=(math.nan, 0.0, 0.0))):
+        with pytest.raises(pace.PaceError) as e:
+            pace.orthogonalize(u, pace.muon_params(**kw))
+        assert e.value.status == pace.ERR_INVALID_ARG, kw
+    with pytest.raises(pace.PaceError) as e:
+        pace.orthogonalize(u, ws=pace.workspace(256, DEV))
+    assert e.value.status == pace.ERR_WORKSPACE
+    with pytest.raises(ValueError, match="float16"):
+        pace.orthogonalize(u.half())
+    with pytest.raises(ValueError, match="contiguous rows"):
+        pace.orthogonalize(u.t())
+    with pytest.raises(ValueError, match="shape"):
+        pace.orthogonalize(u[0])
+    with pytest.raises(ValueError, match="out"):
+        pace.orthogonalize(u, out=torch.zeros(16, 31, device=DEV, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="momentum"):
+        pace.muon_update(u, u, torch.zeros(16, 31, device=DEV))
+    with pytest.raises(ValueError, match="weight"):
+        pace.muon_update(u.bfloat16(), u, u.clone())
+    with pytest.raises(ValueError, match="contiguous"):
+        pace.muon_update(u, u, torch.zeros(32, 16, device=DEV).t())
+    L, fake, q = pace.lib(), 0x1000, pace.muon_params()
+
+    def call(dtype=0, b=1, m=8, n=8, ld=8, out=fake, old=8):
+        return L.pace_orthogonalize(fake, dtype, b, m, n, ld, 64, ctypes.byref(q), out, old, 64,
+                                    fake, 1 << 30, None, None)
+    assert call(dtype=2) == pace.ERR_INVALID_ARG
+    assert call(m=-1) == pace.ERR_INVALID_ARG
+    assert call(m=65537) == pace.ERR_UNSUPPORTED_SHAPE
+    assert call(ld=7) == pace.ERR_INVALID_ARG
+    assert call(old=7) == pace.ERR_INVALID_ARG
+    assert call(out=None) == pace.ERR_INVALID_ARG
+    assert call(out=fake + 1) == pace.ERR_UNSUPPORTED_SHAPE
+    assert call(b=2, m=9) == pace.ERR_INVALID_ARG  # the results of a stack would overlap
