@@ -1,0 +1,459 @@
+// The fused LM head with entropies on few rows (the tokens of a decode step): lp, lse and
+// H as lmhead.cu computes them, bound by reading the vocabulary matrix once.
+//
+// lmhead.cu gives the MMA's M side to the hidden rows, 256 a CTA pair, and reads a hidden
+// tile beside every vocabulary tile; with 8 rows, 31 of 32 rows of the product are padding
+// and every other byte into an SM is too.  Here the operands change places: M is 256
+// vocabulary rows of the pair, N the hidden rows rounded up (16 to 256), each CTA holding
+// half of them.  A stage of the ring is then 16 KB of W and 64 N bytes of hidden states, and
+// eight stages keep 19 MB of W in flight on the chip.
+//
+// few_kernel (CTA pairs, the roles and barriers of lmhead.cu): a pair takes vocabulary tiles
+// cid, cid + pairs, ...  In the epilogue a lane holds one vocabulary row and a register one
+// hidden row, so a tile's softmax sums run over lanes: 32 columns are reduced at once, half
+// as many values left after each of five exchanges, and lane c of a warp keeps the running
+// (m, S, T) of column c.  Warps, then CTAs (few_merge_kernel) are merged at the end.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <float.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <mutex>
+
+#include "pace_internal.cuh"
+#include "pace_loss.cuh"
+#include "pace_tma.cuh"
+
+namespace pace {
+namespace {
+
+constexpr int BM = 128;  // vocabulary rows per CTA; the pair's MMA covers 256
+constexpr int BK = 64;
+constexpr int kThreads = 192;
+constexpr uint32_t kStageW = BM * BK * 2;  // 16 KB
+constexpr int kMaxCtas = 152;
+
+template <int N>
+struct Shape {
+  static constexpr int kRows = N / 2;                    // hidden rows per CTA
+  static constexpr uint32_t kStageH = kRows * BK * 2;
+  static constexpr uint32_t kStage = kStageW + kStageH;
+  static constexpr int kStages = N <= 128 ? 8 : 6;
+  static constexpr int kAcc = N < 32 ? 32 : N;           // columns of an accumulator
+  static constexpr uint32_t kTmemCols = 2 * kAcc;
+  static constexpr int kGroups = kAcc / 32;
+  static constexpr size_t kMerge = 4 * 3 * N * sizeof(float);
+  static constexpr size_t kSmem = 1024 + kStages * kStage + 256 + kMerge;
+};
+
+struct FewArgs {
+  const long long* n_valid_dev;  // rows present (device), or null = rows
+  int rows;                      // at most N
+  int32_t H, V, n_tiles;
+  float scale_log2;              // log2(e) / temperature
+  const int32_t* targets;
+  const int32_t* rowidx;         // compact row -> original row, or null (identity)
+  int gather;                    // 1: hidden rows are read through rowidx
+  float *part_m, *part_s, *part_t;  // [rows][gridDim.x]
+  float* tgt_logit;              // [rows]
+  int32_t* status;
+};
+
+// x[c] summed over the warp's lanes, for c = lane.
+__device__ __forceinline__ float column_sums(float (&x)[32], int lane) {
+#pragma unroll
+  for (int w = 16; w >= 1; w >>= 1) {
+    const bool up = lane & w;
+#pragma unroll
+    for (int i = 0; i < w; ++i) {
+      const float keep = up ? x[i + w] : x[i];
+      const float send = up ? x[i] : x[i + w];
+      x[i] = keep + __shfl_xor_sync(0xffffffffu, send, w);
+    }
+  }
+  return x[0];
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// (m, s, t) <- its sums and (m2, s2, t2)'s against the larger maximum (powers of two).
+__device__ __forceinline__ void merge_sums(float& m, float& s, float& t, float m2, float s2,
+                                           float t2) {
+  const float mn = fmaxf(m, m2);
+  const float d = m - mn, d2 = m2 - mn;
+  const float f = ex2_approx(d), f2 = ex2_approx(d2);
+  t = f * fmaf(d, s, t) + f2 * fmaf(d2, s2, t2);
+  s = f * s + f2 * s2;
+  m = mn;
+}
+
+template <int N>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    few_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_h,
+               FewArgs p) {
+  using S = Shape<N>;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStage);
+  uint64_t* full = bars;
+  uint64_t* empty = bars + S::kStages;
+  uint64_t* tmem_full = bars + 2 * S::kStages;
+  uint64_t* tmem_empty = tmem_full + 2;
+  uint64_t* mma_done = tmem_empty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* merge = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(bars) + 256);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t crank = cluster_ctarank();
+  const bool leader = crank == 0;
+  const int cid = static_cast<int>(blockIdx.x) / 2, n_clusters = static_cast<int>(gridDim.x) / 2;
+  const int n_valid = p.n_valid_dev ? static_cast<int>(*p.n_valid_dev) : p.rows;
+  if (n_valid == 0) return;  // the same in every CTA, before the pair's collective allocation
+  const int nkb = p.H / BK;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tmem_full[b], 1);
+      mbar_init(&tmem_empty[b], 2 * 4);
+    }
+    mbar_init(mma_done, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  cluster_sync();  // both CTAs run and their barriers exist
+  if (warp == 1) {
+    tmem_alloc_pair(tmem_slot, S::kTmemCols);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  cluster_sync();  // both CTAs' tensor memory is allocated before any MMA writes it
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t peer_abort = cluster_addr(const_cast<int*>(abort_flag), crank ^ 1u);
+  auto give_up = [&]() {
+    if (!*abort_flag) report(p.status, PACE_ERR_TIMEOUT);
+    *abort_flag = 1;
+    st_cluster_u32(peer_abort, 1u);
+  };
+
+  if (warp == 0) {
+    // Lane 0 loads the CTA's 128 rows of W, lane 1 its hidden rows as one box; where they
+    // are gathered, lanes 0 .. N / 8 - 1 load four rows each (rows past the count: row 0).
+    uint64_t pol;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+    int32_t g4[4] = {0, 0, 0, 0};
+    if (p.gather && lane < S::kRows / 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = static_cast<int>(crank) * S::kRows + 4 * lane + i;
+        if (c < n_valid) g4[i] = p.rowidx[c];
+      }
+    }
+    uint32_t it = 0;
+    bool ok = true;
+    for (int t = cid; t < p.n_tiles && ok; t += n_clusters) {
+      const int32_t w0 = t * 2 * BM + static_cast<int32_t>(crank) * BM;
+      for (int kb = 0; kb < nkb; ++kb, ++it) {
+        const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1u;
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], ph ^ 1u, abort_flag))) {
+          ok = false;
+          break;
+        }
+        const uint32_t bar = cluster_addr(&full[s], 0);
+        if (leader && lane == 0) mbar_arrive_expect_tx(&full[s], 2 * S::kStage);
+        __syncwarp();  // the lanes' loads are one TMA instruction
+        unsigned char* sw = smem + s * S::kStage;
+        if (p.gather) {
+          if (lane == 0) tma_load_2d_pair(sw, &tm_w, bar, kb * BK, w0, pol);
+          __syncwarp();
+          if (lane < S::kRows / 4)
+            tma_gather4_pair(sw + kStageW + lane * 4 * (BK * 2), &tm_h, bar, kb * BK, g4[0],
+                             g4[1], g4[2], g4[3], pol);
+        } else if (lane < 2) {
+          tma_load_2d_pair(sw + (lane ? kStageW : 0u), lane ? &tm_h : &tm_w, bar, kb * BK,
+                           lane ? static_cast<int32_t>(crank) * S::kRows : w0, pol);
+        }
+      }
+    }
+    if (lane == 0) {
+      if (!ok) give_up();
+      // every copy issued has landed before the CTA exits
+      const uint64_t lim = *abort_flag ? 1000000ull : kWaitLimitNs;
+      for (uint32_t s = 0; s < S::kStages && s < it; ++s) {
+        const uint32_t last = it - 1 - ((it - 1 - s) % S::kStages);
+        if (leader)
+          mbar_wait_bounded(&full[s], (last / S::kStages) & 1u, nullptr, lim);
+        else
+          mbar_wait_bounded(&empty[s], (last / S::kStages) & 1u, nullptr, lim);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && leader) {
+      constexpr uint32_t kIdesc = idesc_bf16_f32(2 * BM, N);
+      uint32_t it = 0, tc = 0;
+      bool ok = true;
+      for (int t = cid; t < p.n_tiles && ok; t += n_clusters, ++tc) {
+        const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
+        if (!mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u, abort_flag)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + acc * S::kAcc;
+        for (int kb = 0; kb < nkb; ++kb, ++it) {
+          const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1u;
+          if (!mbar_wait_bounded(&full[s], ph, abort_flag)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t sw = smem_u32(smem + s * S::kStage);
+#pragma unroll
+          for (int k = 0; k < BK / 16; ++k)
+            tc_mma_f16_pair(d_tmem, smem_desc_k128(sw + k * 32),
+                            smem_desc_k128(sw + kStageW + k * 32), kIdesc,
+                            (kb > 0 || k > 0) ? 1u : 0u);
+          tc_commit_pair(cluster_addr(&empty[s], 0));
+          tc_commit_pair(cluster_addr(&empty[s], 1));
+        }
+        if (!ok) break;
+        tc_commit_pair(cluster_addr(&tmem_full[acc], 0));
+        tc_commit_pair(cluster_addr(&tmem_full[acc], 1));
+      }
+      if (!ok) give_up();
+      tc_commit_pair(cluster_addr(mma_done, 0));
+      mbar_wait_bounded(mma_done, 0, nullptr);
+    }
+  } else {
+    const int quad = warp & 3;
+    const float scale = p.scale_log2;
+    const float outside = fmaxf(-1e30f / scale, -FLT_MAX);  // rows past the vocabulary
+    const uint32_t empty0 = cluster_addr(&tmem_empty[0], 0);
+    const uint32_t empty1 = cluster_addr(&tmem_empty[1], 0);
+    // lane c of group g: hidden row 32 g + c
+    float m[S::kGroups], s[S::kGroups], st[S::kGroups];
+    int32_t y[S::kGroups];
+#pragma unroll
+    for (int g = 0; g < S::kGroups; ++g) {
+      m[g] = -1e30f;
+      s[g] = st[g] = 0.0f;
+      const int c = 32 * g + lane;
+      y[g] = -1;
+      if (c < n_valid) y[g] = p.targets[p.rowidx ? p.rowidx[c] : c];
+    }
+    uint32_t tc = 0;
+    for (int t = cid; t < p.n_tiles; t += n_clusters, ++tc) {
+      const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
+      const bool got = __all_sync(0xffffffffu,
+                                  mbar_wait_bounded(&tmem_full[acc], acc_ph, abort_flag));
+      if (!got) {
+        give_up();
+        break;
+      }
+      tc_fence_after();
+      const int32_t v0 = t * 2 * BM + static_cast<int32_t>(crank) * BM + quad * 32;
+      const bool past = v0 + lane >= p.V;
+      const uint32_t tbase = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + acc * S::kAcc;
+#pragma unroll
+      for (int g = 0; g < S::kGroups; ++g) {
+        if (32 * g >= n_valid) continue;  // the same for the block
+        float v[32];
+        tmem_ld_32x32b_x32(tbase + 32 * g, v);
+        tmem_wait_ld();
+        // columns whose target is one of this warp's 32 vocabulary rows
+        const uint32_t off = static_cast<uint32_t>(y[g] - v0);
+        const uint32_t hits = __ballot_sync(0xffffffffu, off < 32u);
+        if (hits) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (hits >> i & 1u) {
+              const uint32_t from = __shfl_sync(0xffffffffu, off, i);
+              if (static_cast<uint32_t>(lane) == from) p.tgt_logit[32 * g + i] = v[i];
+            }
+        }
+        float mine = 0.0f, e[32], ed[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float u = past ? outside : v[i];
+          const float top = warp_max(u) * scale;
+          const float d = fmaf(u, scale, -top);
+          // (where all rows are past it, d is the rounding of 1e30)
+          e[i] = past ? 0.0f : ex2_approx(d);
+          ed[i] = past ? 0.0f : e[i] * d;
+          if (lane == i) mine = top;
+        }
+        const float sum = column_sums(e, lane), sum_t = column_sums(ed, lane);
+        merge_sums(m[g], s[g], st[g], mine, sum, sum_t);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+    }
+    // the four warps' sums, then this CTA's partial of every row
+    float* mine = merge + quad * 3 * N;
+#pragma unroll
+    for (int g = 0; g < S::kGroups; ++g)
+      if (32 * g + lane < N) {
+        mine[32 * g + lane] = m[g];
+        mine[N + 32 * g + lane] = s[g];
+        mine[2 * N + 32 * g + lane] = st[g];
+      }
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    for (int c = threadIdx.x - 64; c < n_valid; c += 128) {
+      float cm = merge[c], cs = merge[N + c], ct = merge[2 * N + c];
+      for (int w = 1; w < 4; ++w)
+        merge_sums(cm, cs, ct, merge[w * 3 * N + c], merge[w * 3 * N + N + c],
+                   merge[w * 3 * N + 2 * N + c]);
+      const int64_t o = static_cast<int64_t>(c) * gridDim.x + blockIdx.x;
+      p.part_m[o] = cm;
+      p.part_s[o] = cs;
+      p.part_t[o] = ct;
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  // neither CTA frees its tensor memory or leaves while the pair's MMAs, copies
+  // or arrivals may still reach it
+  cluster_sync();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem_base, S::kTmemCols);
+  cluster_sync();  // the collective release is complete in both CTAs
+}
+
+// A warp per row: the CTAs' partials, then lp, lse and the entropy.
+constexpr int kMergeWarps = 8;
+__global__ void __launch_bounds__(kMergeWarps * 32)
+    few_merge_kernel(const long long* __restrict__ n_valid_dev, int rows, int parts, int32_t V,
+                     float inv_temp, const float* __restrict__ part_m,
+                     const float* __restrict__ part_s, const float* __restrict__ part_t,
+                     const float* __restrict__ tgt_logit, const int32_t* __restrict__ targets,
+                     const int32_t* __restrict__ rowidx, float* __restrict__ logprob,
+                     float* __restrict__ lse_out, float* __restrict__ entropy, int32_t* status) {
+  const int lane = threadIdx.x & 31;
+  const int r = static_cast<int>(blockIdx.x) * kMergeWarps + (threadIdx.x >> 5);
+  const int n_valid = n_valid_dev ? static_cast<int>(*n_valid_dev) : rows;
+  if (r >= n_valid) return;
+  const int64_t o = static_cast<int64_t>(r) * parts;
+  float m = -1e30f, s = 0.0f, t = 0.0f;
+  for (int i = lane; i < parts; i += 32) merge_sums(m, s, t, part_m[o + i], part_s[o + i], part_t[o + i]);
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, x);
+    const float s2 = __shfl_xor_sync(0xffffffffu, s, x);
+    const float t2 = __shfl_xor_sync(0xffffffffu, t, x);
+    merge_sums(m, s, t, m2, s2, t2);
+  }
+  if (lane != 0) return;
+  const float l2 = log2f(s);
+  const float lse = (m + l2) * 0.69314718055994531f;
+  const int orig = rowidx ? rowidx[r] : r;
+  const int32_t y = targets[orig];
+  float lp;
+  if (y < 0 || y >= V) {
+    report(status, PACE_ERR_INVALID_ARG);
+    lp = __int_as_float(0x7fc00000);
+  } else {
+    lp = tgt_logit[r] * inv_temp - lse;
+  }
+  logprob[orig] = lp;
+  if (lse_out) lse_out[orig] = lse;
+  entropy[orig] = (l2 - t / s) * 0.69314718055994531f;
+}
+
+// Shared memory opt-in and resident clusters of the current device (cached per device).
+template <int N>
+pace_status few_clusters(int* out) {
+  constexpr int kMaxDevices = 64;
+  static int cached[kMaxDevices];
+  static std::mutex mu;
+  int dev = 0;
+  PACE_TRY_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return PACE_ERR_CUDA;
+  std::lock_guard<std::mutex> g(mu);
+  if (cached[dev] == 0) {
+    PACE_TRY_CUDA(cudaFuncSetAttribute(few_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(Shape<N>::kSmem)));
+    const int n = sm_count() / 2;
+    cached[dev] = n < kMaxCtas / 2 ? (n > 0 ? n : 1) : kMaxCtas / 2;
+  }
+  *out = cached[dev];
+  return PACE_OK;
+}
+
+template <int N>
+pace_status launch_few(const void* hidden, const void* w_vocab, FewArgs a, const LmWs& ws,
+                       float* logprob, float* lse, float* entropy, float temperature,
+                       cudaStream_t st) {
+  CUtensorMap tw, th;
+  PACE_TRY(encode_bf16_2d(&tw, w_vocab, a.V, a.H, a.H, BK, BM));
+  // Listed rows: up to 32, one row a box and four boxes a gather.  More gathers than four a
+  // stage are slower than the stage's 16 KB of W (H 2,048, V 151,936, us a call: 32 rows 112,
+  // 64 rows 144, 128 rows 215), so more rows are copied first (64 rows 116, 128 rows 120).
+  a.gather = a.rowidx && N <= 32 ? 1 : 0;
+  if (a.rowidx && !a.gather) {
+    PACE_TRY(run_gather(hidden, a.H, a.rows, ws.cw, ws.hidden_c, st));
+    hidden = ws.hidden_c;
+  }
+  PACE_TRY(encode_bf16_2d(&th, hidden, a.rows, a.H, a.H, BK, a.gather ? 1 : Shape<N>::kRows));
+  int clusters = 0;
+  PACE_TRY(few_clusters<N>(&clusters));
+  if (clusters > a.n_tiles) clusters = a.n_tiles;
+  const ProfileEvents& pe = profile_events(PACE_PROFILE_LMHEAD);
+  if (pe.begin) PACE_TRY_CUDA(cudaEventRecord(pe.begin, st));
+  few_kernel<N><<<static_cast<unsigned>(2 * clusters), kThreads, Shape<N>::kSmem, st>>>(tw, th, a);
+  PACE_TRY(last_launch_status());
+  if (pe.end) PACE_TRY_CUDA(cudaEventRecord(pe.end, st));
+  few_merge_kernel<<<static_cast<unsigned>((a.rows + kMergeWarps - 1) / kMergeWarps),
+                     kMergeWarps * 32, 0, st>>>(
+      a.n_valid_dev, a.rows, 2 * clusters, a.V, 1.0f / temperature, a.part_m, a.part_s, a.part_t,
+      a.tgt_logit, a.targets, a.rowidx, logprob, lse, entropy, a.status);
+  return last_launch_status();
+}
+
+}  // namespace
+
+bool few_rows(int64_t n_rows, int H) {
+  return n_rows <= kFewRowsMax && (n_rows <= 64 || n_rows <= H / 8);
+}
+
+size_t few_parts(int64_t n_rows) {
+  return static_cast<size_t>(n_rows < kFewRowsMax ? n_rows : kFewRowsMax) * kMaxCtas;
+}
+
+pace_status run_logprob_few(int64_t n_rows, const void* hidden, const void* w_vocab,
+                            const int32_t* targets, int H, int V, float temperature,
+                            float* logprob, float* lse, float* entropy, const LmWs& ws,
+                            const long long* n_valid_dev, const int32_t* rowidx,
+                            int32_t* status_dev, cudaStream_t st) {
+  FewArgs a;
+  a.n_valid_dev = n_valid_dev;
+  a.rows = static_cast<int>(n_rows);
+  a.H = H;
+  a.V = V;
+  a.n_tiles = (V + 2 * BM - 1) / (2 * BM);
+  a.scale_log2 = 1.4426950408889634f / temperature;
+  a.targets = targets;
+  a.rowidx = rowidx;
+  a.part_m = ws.part_m;
+  a.part_s = ws.part_s;
+  a.part_t = ws.part_t;
+  a.tgt_logit = ws.tgt;
+  a.status = status_dev;
+  auto launch = n_rows <= 16 ? launch_few<16> : n_rows <= 32 ? launch_few<32>
+                : n_rows <= 64 ? launch_few<64> : n_rows <= 128 ? launch_few<128> : launch_few<256>;
+  return launch(hidden, w_vocab, a, ws, logprob, lse, entropy, temperature, st);
+}
+
+}  // namespace pace

@@ -959,7 +959,12 @@ void carve_lm_ws(Carver& cv, int64_t n_rows, int64_t n_seq, int H, bool dense_ro
   // partials: of rp row pairs, kMaxSplits a row in the rounds, and C / R + 2 a row
   // for the R row pairs of the tail
   const int64_t rp = (rows_cap + 2 * BM - 1) / (2 * BM);
-  const size_t parts = 2 * BM * (kMaxClusters + static_cast<size_t>(rp) * kMaxSplits);
+  size_t parts = 2 * BM * (kMaxClusters + static_cast<size_t>(rp) * kMaxSplits);
+  if (entropy) {  // what run_logprob_few keeps
+    if (few_parts(n_rows) > parts) parts = few_parts(n_rows);
+    const int64_t rows = n_rows < kFewRowsMax ? n_rows : kFewRowsMax;
+    w->hidden_c = cv.take<uint16_t>(static_cast<size_t>(rows) * H);
+  }
   w->part_m = cv.take<float>(parts);
   w->part_s = cv.take<float>(parts);
   w->tgt = cv.take<float>(static_cast<size_t>(rows_cap));
@@ -969,6 +974,11 @@ void carve_lm_ws(Carver& cv, int64_t n_rows, int64_t n_seq, int H, bool dense_ro
 
 bool lm_needs_compaction(const PaceBatch* b) {
   return b->mask || b->seq_accepted || b->n_rows < BM;
+}
+
+// Whether run_logprob lists the rows (and computes the advantages while it does).
+static bool lm_compacts(const PaceBatch* b, int H, bool entropy) {
+  return entropy && few_rows(b->n_rows, H) ? b->mask || b->seq_accepted : lm_needs_compaction(b);
 }
 
 pace_status check_lm_args(const PaceBatch* batch, const void* hidden, const void* w_vocab,
@@ -992,7 +1002,8 @@ pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* 
                         float* lse, const LmWs& ws, const AdvJob& adv, unsigned* counter,
                         int32_t* status_dev, cudaStream_t st, float* entropy) {
   const int64_t n_rows = batch->n_rows;
-  const bool compact = lm_needs_compaction(batch);
+  const bool few = entropy && few_rows(n_rows, H);
+  const bool compact = lm_compacts(batch, H, entropy != nullptr);
   const long long* n_valid_dev = nullptr;
   const int32_t* rowidx = nullptr;
   int64_t rows_cap = n_rows;
@@ -1005,6 +1016,9 @@ pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* 
     rows_cap = n_rows > BM ? n_rows : BM;
   }
   if (n_rows == 0) return PACE_OK;
+  if (few)
+    return run_logprob_few(n_rows, hidden, w_vocab, targets, H, V, temperature, logprob, lse,
+                           entropy, ws, n_valid_dev, rowidx, status_dev, st);
   const int n_vtiles = (V + BN - 1) / BN;
   LmLaunch l;
   l.hidden = hidden;
@@ -1098,8 +1112,8 @@ pace_status logprob_call(const PaceBatch* batch, const void* hidden, const void*
                        logprob, lse, ws, adv, loss ? ws.sw.counter : nullptr, status_dev, st,
                        entropy));
   if (loss)
-    PACE_TRY(run_surrogate(batch, logprob, loss, ws.sw, lm_needs_compaction(batch), status_dev,
-                           st));
+    PACE_TRY(run_surrogate(batch, logprob, loss, ws.sw, lm_compacts(batch, hidden_size, entropy != nullptr),
+                           status_dev, st));
   return PACE_OK;
 }
 

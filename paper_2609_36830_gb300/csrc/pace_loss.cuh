@@ -68,6 +68,20 @@ pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* 
                         const int32_t* targets, int H, int V, float temperature, float* logprob,
                         float* lse, const LmWs& ws, const AdvJob& adv, unsigned* counter,
                         int32_t* status_dev, cudaStream_t st, float* entropy = nullptr);
+// Log-probs and entropies of at most kFewRowsMax rows (lmfew.cu): of the rows in rowidx,
+// whose number is on the device, or of all n_rows.  few_parts: partials it keeps.
+constexpr int64_t kFewRowsMax = 256;
+// Whether they are to be used: with many rows and short sums their epilogue, which exchanges
+// values between lanes, takes longer than the products (H 256, V 2,048: 100 rows 21 us, 25
+// with lmhead.cu, 200 rows 30 and 19; H 1,024, V 50,001: 128 rows 36 and 57, 256 rows 59 and
+// 56; H 2,048, V 151,936: 256 rows 134 and 178).
+bool few_rows(int64_t n_rows, int H);
+size_t few_parts(int64_t n_rows);
+pace_status run_logprob_few(int64_t n_rows, const void* hidden, const void* w_vocab,
+                            const int32_t* targets, int H, int V, float temperature,
+                            float* logprob, float* lse, float* entropy, const LmWs& ws,
+                            const long long* n_valid_dev, const int32_t* rowidx,
+                            int32_t* status_dev, cudaStream_t st);
 void carve_compact_ws(Carver& cv, int64_t n_rows, CompactWs* w);
 pace_status check_batch(const PaceBatch* b);
 pace_status check_loss_args(const PaceBatch* b, const PaceLossArgs* l);

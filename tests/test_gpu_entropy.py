@@ -45,7 +45,10 @@ def exact(h, w, y, t):
     (1, 64, 1, 1.0, 1.0), (1, 64, 2, 1.0, 1.0), (5, 64, 3, 1.0, 0.7), (8, 256, 2048, 1.0, 1.0),
     (127, 64, 255, 1.0, 1.0), (128, 64, 256, 1.0, 1.3), (129, 192, 257, 0.5, 1.0),
     (300, 1024, 4099, 0.7, 0.7), (2583, 128, 5000, 1.0, 1.0), (4864, 64, 1300, 1.0, 1.0),
-    (20001, 64, 600, 0.9, 1.0), (64, 64, 300, 0.0, 1.0), (600, 64, 50001, 0.5, 1.0)])
+    (20001, 64, 600, 0.9, 1.0), (64, 64, 300, 0.0, 1.0), (600, 64, 50001, 0.5, 1.0),
+    (16, 128, 5000, 1.0, 1.0), (17, 128, 5000, 0.8, 1.0), (32, 2048, 50001, 0.9, 0.7),
+    (33, 64, 20000, 1.0, 1.0), (65, 320, 40001, 0.5, 1.0), (128, 64, 40001, 0.99, 1.0),
+    (200, 192, 39000, 1.0, 1.0), (256, 64, 151936, 0.7, 1.0), (257, 64, 5000, 1.0, 1.0)])
 def test_entropy(rows, H, V, keep, t):
     _, h, w, y, b, inn = make(rows, H, V, keep)
     status = pace.new_status(DEV)
