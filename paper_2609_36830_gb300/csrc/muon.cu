@@ -2,26 +2,28 @@
 //
 // With U a matrix (a gradient, or momentum and gradient), X = U / (|U|_F + eps) and the
 // coefficients (a, b, c),
-//   A = X X^T,  B = b A + c A^2,  X <- a X + B X          `steps` times,
+//   A = X X^T,  C = a I + b A + c A^2,  X <- C X          `steps` times,
 // which drives every singular value of X towards 1 (an odd polynomial of X in its
-// singular values).  For a tall U the same with X^T X and X B, so A and B are s x s, s the
+// singular values).  For a tall U the same with X^T X and X C, so A and C are s x s, s the
 // shorter side, and X is never transposed: the tensor cores read either operand K-major or
 // MN-major.
 //
-// Types.  The operands are fp16 with a power of two beside each (X, A and B are bounded, see
+// Types.  The operands are fp16 with a power of two beside each (X, A and C are bounded, see
 // choose_scales), so they keep 11 significant bits where bf16 has 8: on Gaussian matrices
-// the update is 1.1-1.6e-3 off 64 bits where bf16 products are off 9-13e-3; both run at
-// the same rate.  Sums are fp32, in tensor memory.
+// the update is 1.1-1.5e-3 off 64 bits where bf16 products are off 9-13e-3; both run at
+// the same rate.  Sums are fp32, in tensor memory.  With a I inside C the step's epilogue
+// does not read X again; C's rounding then takes the place of one of a X (as far off 64 bits
+// as without it, on Gaussian matrices and on such with strong directions).
 //
 // newton_schulz_kernel: one cooperative launch does all the products, 3 `steps` phases with
 // a grid barrier between them (a launch for each would add its start and drain to
-// products of 10-100 us).  In a phase the work items are 256 x 256 tiles, dealt to CTA
-// pairs; per pair the structure of the other tensor-core kernels: warp 0 of each CTA issues
-// TMA loads of its 128 A rows and its half of the B tile into a 4-stage ring, warp 1 of the
-// even CTA issues tcgen05.mma.cta_group::2 (M 256, N 256, K 16), warps 2-5 of each CTA
-// drain one of two accumulators while the next tile is computed.  A and B are symmetric, so
-// only tiles on and below the diagonal are computed and each is also stored
-// transposed: 3 s^2 l + s^3 operations a step instead of 4 s^2 l + 2 s^3.
+// products of 5-100 us).  In a phase the work items are 256 x 256 tiles, dealt to CTA
+// pairs (deal_tiles); per pair the structure of the other tensor-core kernels: warp 0 of
+// each CTA issues TMA loads of its 128 A rows and its half of the B tile into a 4-stage
+// ring, warp 1 of the even CTA issues tcgen05.mma.cta_group::2 (M 256, N 256 or 128, K 16),
+// warps 2-9 of each CTA drain one of two accumulators while the next tile is computed.  A
+// and C are symmetric, so only tiles on and below the diagonal are computed and each is
+// also stored transposed: 3 s^2 l + s^3 operations a step instead of 4 s^2 l + 2 s^3.
 // The last phase's epilogue holds the update itself: it is written out in bf16, or goes
 // straight into the weights.
 #include <cuda.h>
@@ -44,35 +46,36 @@ constexpr int TM = 256;  // rows and columns of a pair's tile
 constexpr int BM = 128;  // rows of it per CTA
 constexpr int BK = 64;
 constexpr int STAGES = 4;
-constexpr int kThreads = 192;
+constexpr int kEpiWarps = 8;  // two for each quarter of the tensor memory's lanes
+constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr uint32_t kStageA = BM * BK * 2;      // 16 KB
 constexpr uint32_t kStageB = TM / 2 * BK * 2;  // 16 KB: this CTA's half of the B tile
 constexpr uint32_t kStageBytes = kStageA + kStageB;
 constexpr uint32_t kTmemCols = 2 * TM;
-constexpr uint32_t kOutTile = 32 * 128;        // an epilogue warp's staging tile
-constexpr uint32_t kOutBytes = 4 * 2 * kOutTile;
+constexpr uint32_t kOutTile = 32 * 128;        // an epilogue warp's staging tile, of two
+constexpr uint32_t kOutBytes = kEpiWarps * 2 * kOutTile;
 constexpr size_t kSmemBytes = 1024 + STAGES * kStageBytes + kOutBytes + 256;
 constexpr int kMaxClusters = 76;
 constexpr int kNormBlocks = 128;  // partial sums of a matrix's norm
 
-// A phase's product and what its epilogue makes of it.
-enum { kGram = 0, kPoly = 1, kStep = 2, kLast = 3 };
+// A phase's product.
+enum { kGram = 0, kPoly = 1, kStep = 2 };
 
 struct Maps {
-  CUtensorMap xk[2], xm[2], ak, bk;     // loads: K-major (64 x 128 boxes), MN-major (64 x 64)
-  CUtensorMap xs[2], as, bs, at, bt;    // stores: 32-row tiles, and transposed ones
+  // loads: K-major (64 x 128 and 64 x 64 boxes), MN-major (64 x 64)
+  CUtensorMap xk[2], xk64[2], xm[2], ak, ak64, ck, ck64;
+  CUtensorMap xs[2], as, cs, at, ct;  // stores: 32-row tiles, and transposed ones
 };
 
 struct NsArgs {
   int64_t s, l;            // shorter and longer side
   int batch, steps;
   int tall;                // U has l rows and s columns
-  int64_t ldx, lda;        // row pitch of X, and of A and B
+  int64_t ldx, lda;        // row pitch of X, and of A and C
   int64_t x_rows;          // rows of X
-  __half* x[2];
-  __half *a, *b;
+  __half* a;
   float ca, cb, cc;        // the coefficients
-  float sx, sa, sb;        // powers of two: X, A and B are held times these
+  float sx, sa, sc;        // powers of two: X, A and C are held times these
   unsigned* ctr;           // arrivals at the grid barriers, zero at launch
   int32_t* status;
   // the result: bf16 with strides, or the weights
@@ -99,7 +102,7 @@ __device__ __forceinline__ void fence_proxy_async() {
   asm volatile("fence.proxy.async;" ::: "memory");
 }
 
-// Waits until `target` epilogue warps have arrived; false after kWaitLimitNs or an abort.
+// Waits until `target` CTAs have arrived; false after kWaitLimitNs or an abort.
 __device__ __forceinline__ bool wait_phase(const unsigned* ctr, unsigned target,
                                            volatile int* abort) {
   if (ld_acquire(ctr) >= target) return true;
@@ -113,70 +116,116 @@ __device__ __forceinline__ bool wait_phase(const unsigned* ctr, unsigned target,
   }
 }
 
-// Item t of a phase: its matrix and the tile's row and column.
+// How a phase's tiles are dealt to n_clusters pairs: whole rounds of whole tiles, then the
+// tiles left over, in halves of 128 columns where that fills one round of halves (and takes
+// half the time of a round).
+struct Deal {
+  int64_t full, items;  // whole tiles of the rounds; items in all
+  int halves;           // 2: the tiles left over are dealt as halves
+};
+__host__ __device__ inline Deal deal_tiles(int64_t tiles, int n_clusters) {
+  Deal d;
+  d.full = tiles / n_clusters * n_clusters;
+  const int64_t tail = tiles - d.full;
+  d.halves = 2 * tail <= n_clusters ? 2 : 1;
+  d.items = d.full + tail * d.halves;
+  return d;
+}
+
+// Tiles of a symmetric product (on and below the diagonal), and of the step, in a matrix.
+__host__ __device__ inline int64_t sym_tiles(int64_t s) {
+  const int64_t t = (s + TM - 1) / TM;
+  return t * (t + 1) / 2;
+}
+__host__ __device__ inline int64_t step_tiles(int64_t s, int64_t l) {
+  return ((s + TM - 1) / TM) * ((l + TM - 1) / TM);
+}
+
+// A phase's item: its matrix, the tile's row and column (in 256s), its first column and
+// how many (256 or 128).
 struct Item {
   int z, i, j;
+  int32_t n0, tn;
 };
 
 struct Phase {
   int kind, cur;           // cur: which X is read
-  bool sym;
-  int ti, tj, per;         // tiles of rows and columns, items of a matrix
-  int64_t n_items;
+  bool sym, last;          // last: the epilogue holds the result
+  int ti, tj, per;         // tiles of rows and columns, tiles of a matrix
+  Deal deal;
   int nkb;                 // K steps
-  const CUtensorMap *ma, *mb;
+  int64_t cols;            // of the product
+  const CUtensorMap *ma, *mb, *mb64;
   bool a_mn, b_mn;
 
-  __device__ Phase(const NsArgs& p, const Maps& m, int ph) {
-    const int r = ph % 3, step = ph / 3;
-    kind = r == 2 && step == p.steps - 1 ? kLast : r;
+  __device__ Phase(const NsArgs& p, const Maps& m, int ph, int n_clusters) {
+    kind = ph % 3;
+    const int step = ph / 3;
+    last = kind == kStep && step == p.steps - 1;
     cur = step & 1;
     const int ts = static_cast<int>((p.s + TM - 1) / TM), tl = static_cast<int>((p.l + TM - 1) / TM);
-    sym = r != 2;
+    sym = kind != kStep;
     ti = sym || !p.tall ? ts : tl;
     tj = sym || p.tall ? ts : tl;
     per = sym ? ts * (ts + 1) / 2 : ti * tj;
-    n_items = static_cast<int64_t>(per) * p.batch;
-    nkb = static_cast<int>(((r == 0 ? p.l : p.s) + BK - 1) / BK);
+    deal = deal_tiles(static_cast<int64_t>(per) * p.batch, n_clusters);
+    nkb = static_cast<int>(((kind == kGram ? p.l : p.s) + BK - 1) / BK);
+    cols = sym || p.tall ? p.s : p.l;
     a_mn = b_mn = false;
-    if (r == 0) {
+    if (kind == kGram) {
       ma = mb = p.tall ? &m.xm[cur] : &m.xk[cur];
+      mb64 = p.tall ? &m.xm[cur] : &m.xk64[cur];
       a_mn = b_mn = p.tall;
-    } else if (r == 1) {
+    } else if (kind == kPoly) {
       ma = mb = &m.ak;
+      mb64 = &m.ak64;
     } else if (p.tall) {
       ma = &m.xk[cur];
-      mb = &m.bk;
+      mb = &m.ck;
+      mb64 = &m.ck64;
     } else {
-      ma = &m.bk;
-      mb = &m.xm[cur];
+      ma = &m.ck;
+      mb = mb64 = &m.xm[cur];
       b_mn = true;
     }
   }
 
+  // CTAs that have items: only they write, and arrive at the barrier that ends the phase.
+  __device__ unsigned arrivals(int n_clusters) const {
+    return 2u * static_cast<unsigned>(deal.items < n_clusters ? deal.items : n_clusters);
+  }
+
   __device__ Item item(int64_t t) const {
     Item it;
-    it.z = static_cast<int>(t / per);
-    const int r = static_cast<int>(t - static_cast<int64_t>(it.z) * per);
+    int64_t tile = t;
+    int half = -1;
+    if (t >= deal.full && deal.halves == 2) {
+      tile = deal.full + (t - deal.full) / 2;
+      half = static_cast<int>((t - deal.full) & 1);
+    }
+    it.z = static_cast<int>(tile / per);
+    const int r = static_cast<int>(tile - static_cast<int64_t>(it.z) * per);
     if (sym) {  // row by row of the lower triangle
       int i = static_cast<int>((sqrtf(8.0f * r + 1.0f) - 1.0f) * 0.5f);
       while ((i + 1) * (i + 2) / 2 <= r) ++i;
       while (i * (i + 1) / 2 > r) --i;
       it.i = i;
       it.j = r - i * (i + 1) / 2;
-    } else {  // the shorter side's tiles fastest: a round reads all of B and part of X
+    } else {  // the shorter side's tiles fastest: a round reads all of C and part of X
       const bool rows_fast = ti <= tj;
       it.i = rows_fast ? r % ti : r / tj;
       it.j = rows_fast ? r / ti : r % tj;
     }
+    it.n0 = it.j * TM + (half > 0 ? TM / 2 : 0);
+    it.tn = half >= 0 ? TM / 2 : TM;
     return it;
   }
 };
 
-// fp16 operands, fp32 sums, M 256, N 256.
-__device__ __forceinline__ uint32_t idesc_f16(bool a_mn, bool b_mn) {
+// fp16 operands, fp32 sums, M 256.
+__device__ __forceinline__ uint32_t idesc_f16(int32_t n, bool a_mn, bool b_mn) {
   return (1u << 4) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-         ((static_cast<uint32_t>(TM) >> 3) << 17) | ((static_cast<uint32_t>(TM) >> 4) << 24);
+         ((static_cast<uint32_t>(n) >> 3) << 17) | ((static_cast<uint32_t>(TM) >> 4) << 24);
 }
 
 __device__ __forceinline__ uint32_t half2_rn(float lo, float hi) {
@@ -185,23 +234,76 @@ __device__ __forceinline__ uint32_t half2_rn(float lo, float hi) {
   return r;
 }
 
-// 32 fp16 values of a row (64 bytes, aligned) as floats.
-__device__ __forceinline__ void load_row32(const __half* src, float (&f)[32]) {
+__device__ __forceinline__ float2 half2_value(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+
+// Rows of a 32 x 32 block of the result, from the warp's staging tile: W and its copy,
+// or the bf16 update.  `w` holds the weights asked for earlier (load_weights).
+struct Block {
+  int64_t row0, rows, col0, cols;
+  int z;
+};
+
+__device__ __forceinline__ void load_weights(const NsArgs& p, const Block& b, int lane,
+                                             float4 (&w)[8]) {
+  const int64_t col = b.col0 + 4 * (lane & 7);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const uint4 u = __ldcg(reinterpret_cast<const uint4*>(src) + q);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  for (int k = 0; k < 8; ++k) {
+    const int64_t row = b.row0 + 4 * k + (lane >> 3);
+    if (row < b.rows && col < b.cols)
+      w[k] = *reinterpret_cast<const float4*>(p.weight + (b.z * b.rows + row) * b.cols + col);
+  }
+}
+
+__device__ __forceinline__ void store_result4(const NsArgs& p, const Block& b, int lane,
+                                              const float* tile, float4 (&w)[8]) {
+  const int q = lane & 7;
+  const int64_t col = b.col0 + 4 * q;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      f[8 * q + 2 * i] = p.x;
-      f[8 * q + 2 * i + 1] = p.y;
+  for (int k = 0; k < 8; ++k) {
+    const int r = 4 * k + (lane >> 3);
+    const int64_t row = b.row0 + r;
+    if (row >= b.rows || col >= b.cols) continue;
+    const float4 o = *reinterpret_cast<const float4*>(tile + r * 32 + ((q ^ (r & 7)) << 2));
+    if (p.weight) {
+      const int64_t at = (b.z * b.rows + row) * b.cols + col;
+      const float4 v = make_float4(
+          fmaf(w[k].x, p.keep, -p.rate * o.x), fmaf(w[k].y, p.keep, -p.rate * o.y),
+          fmaf(w[k].z, p.keep, -p.rate * o.z), fmaf(w[k].w, p.keep, -p.rate * o.w));
+      *reinterpret_cast<float4*>(p.weight + at) = v;
+      if (p.weight16)
+        *reinterpret_cast<uint2*>(p.weight16 + at) =
+            make_uint2(bf16x2_rn(v.x, v.y), bf16x2_rn(v.z, v.w));
+    } else {
+      *reinterpret_cast<uint2*>(p.out + b.z * p.out_bs + row * p.out_ld + col) =
+          make_uint2(bf16x2_rn(o.x, o.y), bf16x2_rn(o.z, o.w));
+    }
+  }
+}
+
+__device__ __forceinline__ void store_result1(const NsArgs& p, const Block& b, int lane,
+                                              const float* tile) {
+  const int64_t col = b.col0 + lane;
+  if (col >= b.cols) return;
+#pragma unroll 4
+  for (int r = 0; r < 32; ++r) {
+    const int64_t row = b.row0 + r;
+    if (row >= b.rows) break;
+    const float o = tile[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
+    if (p.weight) {
+      const int64_t at = (b.z * b.rows + row) * b.cols + col;
+      const float v = fmaf(p.weight[at], p.keep, -p.rate * o);
+      p.weight[at] = v;
+      if (p.weight16) p.weight16[at] = __float2bfloat16_rn(v);
+    } else {
+      p.out[b.z * p.out_bs + row * p.out_ld + col] = __float2bfloat16_rn(o);
     }
   }
 }
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    newton_schulz_kernel(const __grid_constant__ Maps maps, const NsArgs p) {
+    newton_schulz_kernel(const __grid_constant__ Maps maps, const __grid_constant__ NsArgs p) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -211,15 +313,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   uint64_t* tmem_full = bars + 2 * STAGES;
   uint64_t* tmem_empty = tmem_full + 2;
   uint64_t* mma_done = tmem_empty + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(mma_done + 1);
+  uint64_t* opened = mma_done + 1;  // [1] the phase's inputs are written (producer -> epilogue)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(opened + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t crank = cluster_ctarank();
   const bool leader = crank == 0;
-  const int64_t cid = blockIdx.x / 2, n_clusters = gridDim.x / 2;
+  const int cid = static_cast<int>(blockIdx.x) / 2, n_clusters = static_cast<int>(gridDim.x) / 2;
   const int n_phases = 3 * p.steps;
-  const unsigned arrivals = gridDim.x * 4;  // epilogue warps of a phase
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -228,9 +330,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&tmem_full[b], 1);
-      mbar_init(&tmem_empty[b], 2 * 4);  // one arrival per epilogue warp of the pair
+      mbar_init(&tmem_empty[b], 2 * kEpiWarps);  // one arrival per epilogue warp of the pair
     }
     mbar_init(mma_done, 1);
+    mbar_init(opened, 1);
     *abort_flag = 0;
     fence_barrier_init();
   }
@@ -254,28 +357,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     uint64_t pol;
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
     uint32_t it = 0;
+    unsigned before = 0;  // arrivals of the phases before this one
     bool ok = true;
     for (int ph = 0; ph < n_phases && ok; ++ph) {
-      const Phase f(p, maps, ph);
-      if (ph > 0) {  // what this phase reads is written
-        const bool go = lane != 0 || wait_phase(p.ctr, ph * arrivals, abort_flag);
+      const Phase f(p, maps, ph, n_clusters);
+      if (cid < f.deal.items) {
+        // what this phase reads is written
+        const bool go = lane != 0 || ph == 0 || wait_phase(p.ctr, before, abort_flag);
         if (!__all_sync(0xffffffffu, go)) {
           ok = false;
           break;
         }
         fence_proxy_async();
+        if (lane == 0) mbar_arrive(opened);
       }
-      const int boxes_a = f.a_mn ? 2 : 1, boxes = boxes_a + (f.b_mn ? 2 : 1);
+      before += f.arrivals(n_clusters);
+      const int boxes_a = f.a_mn ? 2 : 1;
       const bool is_a = lane < boxes_a;
-      const int half = is_a ? lane : lane - boxes_a;  // which 64-wide box of an MN-major tile
-      const CUtensorMap* desc = is_a ? f.ma : f.mb;
+      const int box = is_a ? lane : lane - boxes_a;  // which 64-wide box of an MN-major tile
       const bool mn = is_a ? f.a_mn : f.b_mn;
-      const uint32_t dst = (is_a ? 0u : kStageA) + half * 8192u;
-      for (int64_t t = cid; t < f.n_items && ok; t += n_clusters) {
+      const uint32_t dst = (is_a ? 0u : kStageA) + box * 8192u;
+      for (int64_t t = cid; t < f.deal.items && ok; t += n_clusters) {
         const Item im = f.item(t);
-        const int32_t r0 = (is_a ? im.i * TM : im.j * TM) + static_cast<int32_t>(crank) * BM;
-        const int32_t x = mn ? r0 + 64 * half : 0, dx = mn ? 0 : BK;
+        if (im.n0 >= f.cols) continue;  // the second half of a narrow last tile
+        const int boxes = boxes_a + (f.b_mn ? im.tn / 128 : 1);
+        const CUtensorMap* desc = is_a ? f.ma : im.tn == TM ? f.mb : f.mb64;
+        const int32_t r0 = is_a ? im.i * TM + static_cast<int32_t>(crank) * BM
+                                : im.n0 + static_cast<int32_t>(crank) * (im.tn / 2);
+        const int32_t x = mn ? r0 + 64 * box : 0, dx = mn ? 0 : BK;
         const int32_t y = mn ? 0 : r0, dy = mn ? BK : 0;
+        const uint32_t bytes = 2 * (kStageA + im.tn * BK);
         for (int kb = 0; kb < f.nkb; ++kb, ++it) {
           const uint32_t s = it % STAGES, par = (it / STAGES) & 1u;
           if (!__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], par ^ 1u, abort_flag))) {
@@ -283,7 +394,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             break;
           }
           const uint32_t bar = cluster_addr(&full[s], 0);
-          if (leader && lane == 0) mbar_arrive_expect_tx(&full[s], 2 * kStageBytes);
+          if (leader && lane == 0) mbar_arrive_expect_tx(&full[s], bytes);
           __syncwarp();  // the lanes' loads are one TMA instruction
           if (lane < boxes)
             tma_load_3d_pair(smem + s * kStageBytes + dst, desc, bar, x + kb * dx, y + kb * dy,
@@ -308,11 +419,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       uint32_t it = 0, tc = 0;
       bool ok = true;
       for (int ph = 0; ph < n_phases && ok; ++ph) {
-        const Phase f(p, maps, ph);
-        const uint32_t idesc = idesc_f16(f.a_mn, f.b_mn);
+        const Phase f(p, maps, ph, n_clusters);
         const uint32_t da = f.a_mn ? 2048 : 32, db = f.b_mn ? 2048 : 32;
-        for (int64_t t = cid; t < f.n_items && ok; t += n_clusters, ++tc) {
+        for (int64_t t = cid; t < f.deal.items && ok; t += n_clusters) {
+          const Item im = f.item(t);
+          if (im.n0 >= f.cols) continue;
+          const uint32_t idesc = idesc_f16(im.tn, f.a_mn, f.b_mn);
           const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
+          ++tc;
           if (!mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u, abort_flag)) {
             ok = false;
             break;
@@ -346,44 +460,59 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       mbar_wait_bounded(mma_done, 0, nullptr);
     }
   } else {
-    const int quad = warp & 3;
+    // Epilogue: warps w and w + 4 share a quarter of the lanes (32 rows) and take half of the
+    // tile's columns each.
+    const int quad = warp & 3, side = (warp - 2) >> 2;
     const uint32_t empty0 = cluster_addr(&tmem_empty[0], 0);
     const uint32_t empty1 = cluster_addr(&tmem_empty[1], 0);
     unsigned char* stage = smem + STAGES * kStageBytes + (warp - 2) * 2 * kOutTile;
-    uint32_t tc = 0;
+    uint32_t tc = 0, n_out = 0, n_open = 0;
     bool ok = true;
     for (int ph = 0; ph < n_phases && ok; ++ph) {
-      const Phase f(p, maps, ph);
-      if (ph > 0) {  // A and X of earlier phases are read below
-        const bool go = lane != 0 || wait_phase(p.ctr, ph * arrivals, abort_flag);
-        if (!__all_sync(0xffffffffu, go)) {
-          give_up();
-          ok = false;
-          break;
-        }
+      const Phase f(p, maps, ph, n_clusters);
+      if (cid >= f.deal.items) continue;
+      // A is read below
+      if (!__all_sync(0xffffffffu, mbar_wait_bounded(opened, n_open & 1u, abort_flag))) {
+        give_up();
+        ok = false;
+        break;
       }
+      ++n_open;
       const int64_t rows = f.sym ? p.s : p.x_rows;
-      const int64_t cols = f.sym || p.tall ? p.s : p.l;
-      const __half* src = f.kind == kPoly ? p.a : p.x[f.cur];
-      const int64_t ld = f.kind == kPoly ? p.lda : p.ldx;
-      const CUtensorMap* store = f.kind == kGram ? &maps.as : f.kind == kPoly ? &maps.bs
-                                                                             : &maps.xs[f.cur ^ 1];
-      const CUtensorMap* mirror = f.kind == kGram ? &maps.at : &maps.bt;
-      // value = f_acc * accumulator + f_src * source
-      float f_acc, f_src = 0.0f;
+      const CUtensorMap* store =
+          f.kind == kGram ? &maps.as : f.kind == kPoly ? &maps.cs : &maps.xs[f.cur ^ 1];
+      const CUtensorMap* mirror = f.kind == kGram ? &maps.at : &maps.ct;
+      // value = f_acc * accumulator (+ f_src * A + diag on the diagonal)
+      float f_acc, f_src = 0.0f, diag = 0.0f;
       if (f.kind == kGram) {
         f_acc = p.sa / (p.sx * p.sx);
       } else if (f.kind == kPoly) {
-        f_acc = p.cc * p.sb / (p.sa * p.sa);
-        f_src = p.cb * p.sb / p.sa;
+        f_acc = p.cc * p.sc / (p.sa * p.sa);
+        f_src = p.cb * p.sc / p.sa;
+        diag = p.ca * p.sc;
       } else {
-        const float unit = f.kind == kLast ? 1.0f / p.sx : 1.0f;
-        f_acc = unit / p.sb;
-        f_src = unit * p.ca;
+        f_acc = f.last ? 1.0f / (p.sc * p.sx) : 1.0f / p.sc;
       }
-      for (int64_t t = cid; t < f.n_items; t += n_clusters, ++tc) {
+      for (int64_t t = cid; t < f.deal.items; t += n_clusters) {
         const Item im = f.item(t);
+        if (im.n0 >= f.cols) continue;
         const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
+        ++tc;
+        const int64_t row_w = static_cast<int64_t>(im.i) * TM + crank * BM + quad * 32;
+        const int64_t row = row_w + lane;
+        const int c_begin = side * (im.tn / 2), c_end = c_begin + im.tn / 2;
+        // A's entries (of 64 columns) are on their way while the product is computed
+        uint4 src[8];
+        const __half* a_row = p.a + (static_cast<int64_t>(im.z) * p.s + row) * p.lda + im.n0;
+        auto load_a = [&](int c0) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            src[q] = make_uint4(0, 0, 0, 0);
+            if (row < rows && im.n0 + c0 + 8 * q < f.cols)
+              src[q] = __ldcg(reinterpret_cast<const uint4*>(a_row + c0 + 8 * q));
+          }
+        };
+        if (f.kind == kPoly) load_a(c_begin);
         const bool got = __all_sync(0xffffffffu,
                                     mbar_wait_bounded(&tmem_full[acc], acc_ph, abort_flag));
         if (!got) {
@@ -392,138 +521,120 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           break;
         }
         tc_fence_after();
-        const int64_t row_w = static_cast<int64_t>(im.i) * TM + crank * BM + quad * 32;
-        const int64_t row = row_w + lane;
         const uint32_t tbase = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + acc * TM;
-        const __half* srow = src + (static_cast<int64_t>(im.z) * rows + row) * ld;
+        if (!f.last) {
 #pragma unroll 1
-        for (int c = 0; c < TM; c += 32) {
-          const int64_t col0 = static_cast<int64_t>(im.j) * TM + c;
-          if (row_w >= rows || col0 >= cols) break;  // the same for the warp; later columns too
-          float v[32];
-          tmem_ld_32x32b_x32(tbase + c, v);
-          float x[32];
-          if (f.kind != kGram) {
-            if (row < rows) {
-              load_row32(srow + col0, x);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = 0.0f;
-            }
-          }
-          tmem_wait_ld();
-          if (f.kind == kGram) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= f_acc;
-          } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], f_acc, x[i] * f_src);
-          }
-          if (f.kind != kLast) {
+          for (int c0 = c_begin; c0 < c_end; c0 += 64) {
+            const int64_t col0 = im.n0 + c0;
+            // the same for the warp; and later columns are outside too
+            if (row_w >= rows || col0 >= f.cols) break;
+            if (f.kind == kPoly && c0 != c_begin) load_a(c0);
             // 32 rows x 64 columns leave as one TMA tile of 128-byte rows (128-byte
-            // swizzle: the lanes' 16-byte stores are conflict-free)
-            if ((c & 32) == 0) {
-              if (lane == 0) bulk_wait_read<0>();
-              __syncwarp();
+            // swizzle: the lanes' 16-byte stores are conflict-free), and transposed as 64
+            // rows of 32
+            const bool flip = f.sym && im.i != im.j;
+            if (lane == 0) {
+              if (f.sym) bulk_wait_read<0>();
+              else bulk_wait_read<1>();
             }
-            uint32_t h[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i], v[2 * i + 1]);
-            unsigned char* orow = stage + lane * 128;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int at = (c & 32 ? 4 : 0) + q;
-              *reinterpret_cast<uint4*>(orow + ((at ^ (lane & 7)) << 4)) =
-                  make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
-            }
-            if (f.sym && im.i != im.j) {  // and transposed: 64 rows of 32
-              uint16_t* tcol =
-                  reinterpret_cast<uint16_t*>(stage + kOutTile) + (c & 32) * 32 + lane;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                tcol[(2 * i) * 32] = static_cast<uint16_t>(h[i] & 0xffffu);
-                tcol[(2 * i + 1) * 32] = static_cast<uint16_t>(h[i] >> 16);
-              }
-            }
-            if ((c & 32) || col0 + 32 >= cols) {
-              fence_proxy_async_smem();
-              __syncwarp();
-              if (lane == 0) {
-                const int32_t cb = static_cast<int32_t>(col0 & ~int64_t{63});
-                tma_store_3d(store, stage, cb, static_cast<int32_t>(row_w), im.z);
-                if (f.sym && im.i != im.j)
-                  tma_store_3d(mirror, stage + kOutTile, static_cast<int32_t>(row_w), cb, im.z);
-                bulk_commit();
-              }
-            }
-          } else {
-            // The update.  Through shared memory, so that the warp's accesses to the
-            // result are whole rows of its 32 x 32 block.
             __syncwarp();
-            float* tile = reinterpret_cast<float*>(stage);
+            unsigned char* tile = stage + (flip ? 0u : (n_out++ & 1u) * kOutTile);
+            uint16_t* tcol = reinterpret_cast<uint16_t*>(stage + kOutTile) + lane;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float v[32];
+              tmem_ld_32x32b_x32(tbase + c0 + 32 * k, v);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] *= f_acc;
+              if (f.kind == kPoly) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                  const uint4 u = src[4 * k + q];
+                  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    const float2 x = half2_value(w[i]);
+                    v[8 * q + 2 * i] = fmaf(x.x, f_src, v[8 * q + 2 * i]);
+                    v[8 * q + 2 * i + 1] = fmaf(x.y, f_src, v[8 * q + 2 * i + 1]);
+                  }
+                }
+                if (row_w == col0 + 32 * k) {  // the diagonal passes through this block
+#pragma unroll
+                  for (int i = 0; i < 32; ++i)
+                    if (lane == i) v[i] += diag;
+                }
+              }
+              uint32_t h[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<uint4*>(tile + lane * 128 + (((4 * k + q) ^ (lane & 7)) << 4)) =
+                    make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+              if (flip) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  tcol[(32 * k + 2 * i) * 32] = static_cast<uint16_t>(h[i] & 0xffffu);
+                  tcol[(32 * k + 2 * i + 1) * 32] = static_cast<uint16_t>(h[i] >> 16);
+                }
+              }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_3d(store, tile, static_cast<int32_t>(col0), static_cast<int32_t>(row_w),
+                           im.z);
+              if (flip)
+                tma_store_3d(mirror, stage + kOutTile, static_cast<int32_t>(row_w),
+                             static_cast<int32_t>(col0), im.z);
+              bulk_commit();
+            }
+          }
+        } else {
+          // The update.  Through shared memory, so that the warp's accesses to the
+          // result are whole rows of its 32 x 32 blocks.
+          float* tile = reinterpret_cast<float*>(stage);
+          Block b{row_w, rows, 0, f.cols, im.z};
+#pragma unroll 1
+          for (int c = c_begin; c < c_end; c += 32) {
+            b.col0 = im.n0 + c;
+            if (row_w >= rows || b.col0 >= f.cols) break;
+            float4 w[8];
+            if (p.vec && p.weight) load_weights(p, b, lane, w);
+            float v[32];
+            tmem_ld_32x32b_x32(tbase + c, v);
+            tmem_wait_ld();
+            __syncwarp();
 #pragma unroll
             for (int q = 0; q < 8; ++q)
               *reinterpret_cast<float4*>(tile + lane * 32 + ((q ^ (lane & 7)) << 2)) =
-                  make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                  make_float4(v[4 * q] * f_acc, v[4 * q + 1] * f_acc, v[4 * q + 2] * f_acc,
+                              v[4 * q + 3] * f_acc);
             __syncwarp();
-            const int64_t z_row = static_cast<int64_t>(im.z) * rows + row_w;
-            if (p.vec) {  // 4 columns a lane: columns are a multiple of 4
-              const int q = lane & 7;
-              const int64_t col = col0 + 4 * q;
-#pragma unroll 1
-              for (int r = lane >> 3; r < 32; r += 4) {
-                if (row_w + r >= rows || col >= cols) continue;
-                const float4 o =
-                    *reinterpret_cast<const float4*>(tile + r * 32 + ((q ^ (r & 7)) << 2));
-                if (p.weight) {
-                  const int64_t at = (z_row + r) * cols + col;
-                  float4* w4 = reinterpret_cast<float4*>(p.weight + at);
-                  float4 w = *w4;
-                  w.x = fmaf(w.x, p.keep, -p.rate * o.x);
-                  w.y = fmaf(w.y, p.keep, -p.rate * o.y);
-                  w.z = fmaf(w.z, p.keep, -p.rate * o.z);
-                  w.w = fmaf(w.w, p.keep, -p.rate * o.w);
-                  *w4 = w;
-                  if (p.weight16)
-                    *reinterpret_cast<uint2*>(p.weight16 + at) =
-                        make_uint2(bf16x2_rn(w.x, w.y), bf16x2_rn(w.z, w.w));
-                } else {
-                  *reinterpret_cast<uint2*>(p.out + im.z * p.out_bs + (row_w + r) * p.out_ld +
-                                            col) =
-                      make_uint2(bf16x2_rn(o.x, o.y), bf16x2_rn(o.z, o.w));
-                }
-              }
-            } else {  // a column a lane
-              const int64_t col = col0 + lane;
-#pragma unroll 1
-              for (int r = 0; r < 32 && row_w + r < rows; ++r) {
-                if (col >= cols) continue;
-                const float o = tile[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
-                if (p.weight) {
-                  const int64_t at = (z_row + r) * cols + col;
-                  const float w = fmaf(p.weight[at], p.keep, -p.rate * o);
-                  p.weight[at] = w;
-                  if (p.weight16) p.weight16[at] = __float2bfloat16_rn(w);
-                } else {
-                  p.out[im.z * p.out_bs + (row_w + r) * p.out_ld + col] = __float2bfloat16_rn(o);
-                }
-              }
-            }
+            if (p.vec)
+              store_result4(p, b, lane, tile, w);
+            else
+              store_result1(p, b, lane, tile);
           }
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
       }
-      // this warp's tiles are in memory: the next phase may read them
+      // the CTA's tiles are in memory: one arrival for it, and the next phase may read them
       if (lane == 0) {
         bulk_wait_all();
         fence_proxy_async();
-        __threadfence();
-        if (ok) red_release(p.ctr);
       }
-      __syncwarp();
+      asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
+      if (warp == 2 && lane == 0 && !*abort_flag) {
+        __threadfence();
+        red_release(p.ctr);
+      }
     }
+    if (lane == 0) bulk_wait_all();
+    __syncwarp();
   }
 
   tc_fence_before();
@@ -674,7 +785,7 @@ __global__ void __launch_bounds__(kElemThreads) direction_kernel(const UArgs p) 
 // ------------------------------------------------------------- host side
 
 struct MuonWs {
-  __half *x[2], *a, *b;
+  __half *x[2], *a, *c;
   double* partial;
   unsigned* ctr;
   int64_t ldx, lda;
@@ -688,12 +799,12 @@ void carve_muon_ws(Carver& cv, int64_t batch, int64_t rows, int64_t cols, MuonWs
   const size_t na = static_cast<size_t>(batch) * s * w->lda;
   for (int i = 0; i < 2; ++i) w->x[i] = cv.take<__half>(nx);
   w->a = cv.take<__half>(na);
-  w->b = cv.take<__half>(na);
+  w->c = cv.take<__half>(na);
   w->partial = cv.take<double>(static_cast<size_t>(batch) * kNormBlocks);
   w->ctr = cv.take<unsigned>(1);
 }
 
-// The largest |a x + b x^3 + c x^5| (odd) or |b x + c x^2| over 0 <= x <= r.
+// The largest |a x + b x^3 + c x^5| over 0 <= x <= r.
 double largest_step(double a, double b, double c, double r) {
   auto f = [&](double x) { return fabs(x * (a + x * x * (b + c * x * x))); };
   double m = f(r);
@@ -709,17 +820,19 @@ double largest_step(double a, double b, double c, double r) {
   }
   return m;
 }
-double largest_poly(double b, double c, double r) {
-  double m = fabs(r * (b + c * r));
+// The largest |a + b y + c y^2| over 0 <= y <= r.
+double largest_poly(double a, double b, double c, double r) {
+  auto f = [&](double y) { return fabs(a + y * (b + c * y)); };
+  double m = fmax(f(0.0), f(r));
   const double y = c != 0 ? -b / (2 * c) : -1;
-  if (y > 0 && y < r) m = fmax(m, fabs(y * (b + c * y)));
+  if (y > 0 && y < r) m = fmax(m, f(y));
   return m;
 }
 
-// Powers of two that keep X, A and B inside fp16 and as far up in it as they can be.  X's
+// Powers of two that keep X, A and C inside fp16 and as far up in it as they can be.  X's
 // singular values start at most 1 (its Frobenius norm is) and a step maps them by the odd
 // polynomial, so its largest value R over all steps bounds X's entries, R^2 those of A and
-// the quadratic's largest value over [0, R^2] those of B.  1 % more at every step and 5 %
+// the quadratic's largest value over [0, R^2] those of C.  1 % more at every step and 5 %
 // at the end for rounding.
 bool choose_scales(const PaceMuonParams* q, NsArgs* p) {
   double r = 1.0, most = 1.0;
@@ -733,7 +846,7 @@ bool choose_scales(const PaceMuonParams* q, NsArgs* p) {
   };
   p->sx = scale(1.05 * most);
   p->sa = scale(1.05 * most * most);
-  p->sb = scale(1.05 * largest_poly(q->coef[1], q->coef[2], 1.05 * most * most));
+  p->sc = scale(1.05 * largest_poly(q->coef[0], q->coef[1], q->coef[2], 1.05 * most * most));
   return true;
 }
 
@@ -808,28 +921,31 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
   n.steps = q->steps;
   n.ldx = w.ldx;
   n.lda = w.lda;
-  n.x[0] = w.x[0];
-  n.x[1] = w.x[1];
   n.a = w.a;
-  n.b = w.b;
   n.ca = q->coef[0];
   n.cb = q->coef[1];
   n.cc = q->coef[2];
   n.ctr = w.ctr;
 
   Maps m;
-  const int64_t xbs = u.rows * w.ldx, abs_ = n.s * w.lda;
+  const int64_t xbs = u.rows * w.ldx, cbs = n.s * w.lda;
   for (int i = 0; i < 2; ++i) {
-    PACE_TRY(encode_f16_3d(&m.xk[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, BM, true));
-    PACE_TRY(encode_f16_3d(&m.xm[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 64, true));
+    PACE_TRY(encode_f16_3d(&m.xk[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 128, true));
+    PACE_TRY(encode_f16_3d(&m.xk64[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 64, true));
     PACE_TRY(encode_f16_3d(&m.xs[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 32, true));
+    m.xm[i] = m.xk64[i];
   }
-  PACE_TRY(encode_f16_3d(&m.ak, w.a, batch, n.s, n.s, w.lda, abs_, 64, BM, true));
-  PACE_TRY(encode_f16_3d(&m.bk, w.b, batch, n.s, n.s, w.lda, abs_, 64, BM, true));
-  PACE_TRY(encode_f16_3d(&m.as, w.a, batch, n.s, n.s, w.lda, abs_, 64, 32, true));
-  PACE_TRY(encode_f16_3d(&m.bs, w.b, batch, n.s, n.s, w.lda, abs_, 64, 32, true));
-  PACE_TRY(encode_f16_3d(&m.at, w.a, batch, n.s, n.s, w.lda, abs_, 32, 64, false));
-  PACE_TRY(encode_f16_3d(&m.bt, w.b, batch, n.s, n.s, w.lda, abs_, 32, 64, false));
+  auto square = [&](CUtensorMap* tm, __half* at, int inner, int outer, bool swizzle) {
+    return encode_f16_3d(tm, at, batch, n.s, n.s, w.lda, cbs, inner, outer, swizzle);
+  };
+  PACE_TRY(square(&m.ak, w.a, 64, 128, true));
+  PACE_TRY(square(&m.ak64, w.a, 64, 64, true));
+  PACE_TRY(square(&m.as, w.a, 64, 32, true));
+  PACE_TRY(square(&m.at, w.a, 32, 64, false));
+  PACE_TRY(square(&m.ck, w.c, 64, 128, true));
+  PACE_TRY(square(&m.ck64, w.c, 64, 64, true));
+  PACE_TRY(square(&m.cs, w.c, 64, 32, true));
+  PACE_TRY(square(&m.ct, w.c, 32, 64, false));
 
   int max_clusters = 0;
   PACE_TRY(ns_max_clusters(&max_clusters));
@@ -840,9 +956,9 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
   direction_kernel<false><<<egrid, kElemThreads, 0, st>>>(u);
   PACE_TRY(last_launch_status());
 
-  const int64_t ts = (n.s + TM - 1) / TM, tl = (n.l + TM - 1) / TM;
-  const int64_t items = batch * (ts * tl > ts * (ts + 1) / 2 ? ts * tl : ts * (ts + 1) / 2);
-  const int64_t clusters = items < max_clusters ? items : max_clusters;
+  // as many pairs as the phase of most items can use (its tiles as halves)
+  const int64_t tiles = step_tiles(n.s, n.l) > sym_tiles(n.s) ? step_tiles(n.s, n.l) : sym_tiles(n.s);
+  const int64_t clusters = 2 * batch * tiles < max_clusters ? 2 * batch * tiles : max_clusters;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(2 * clusters), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
