@@ -8,12 +8,15 @@
 // lane keeps (m, S, T) over its logits and rescales them when its maximum grows.
 //
 // Alternatives without a second pass: the row is cut into chunks of 32 vectors of 16
-// bytes (one load of a warp), whose maxima the pass has at hand.  A logit among the k
-// first (by value, equal ones lowest place first) lies in one of the k first chunks
-// (by maximum, equal ones lowest first): every chunk before its own holds a logit
-// before it.  The same holds for the 16-byte vectors of those chunks, and for the
-// logits of the k first vectors.  So k chunks are read again, then k vectors: 512 k
-// bytes of a row's 300 KB, and nothing depends on how many logits are equal.
+// bytes (one load of a warp), whose maxima the pass has at hand.  The k-th largest of the
+// maxima of disjoint groups of lanes is a bound that k logits reach, so every logit of the
+// k first lies in a chunk whose maximum reaches it.  As a rule these are hardly more than k
+// chunks and k logits: they are read again (512 k of a row's 300 KB) and ranked by counting.
+// Where equal logits make them many (more than kMaxListed chunks or kMaxCand logits), the
+// same is done exactly: a logit among the k first (by value, equal ones lowest place first)
+// lies in one of the k first chunks (by maximum, equal ones lowest first), since every chunk
+// before its own holds a logit before it, and so for the 16-byte vectors of those chunks
+// and the logits of the k first vectors.
 #include <float.h>
 #include <math.h>
 
@@ -31,16 +34,31 @@ constexpr int kTopMax = 64;
 constexpr int kMaxWarps = 8;
 constexpr int kMaxCluster = 8;
 constexpr int kUnroll = 4;             // chunks a warp has in flight
+constexpr int kMaxListed = 256;        // chunks that reach the bound, as a rule about k
+constexpr int kMaxCand = 512;          // logits that do
 constexpr uint32_t kNoPlace = 0x007FFFFFu;  // order_key(-inf)
 constexpr float kLog2e = 1.4426950408889634f;
 
 // ------------------------------------------------------------- logit types
 
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 template <typename T>
 struct Logit;
 template <>
 struct Logit<float> {
+  static constexpr bool kPacked = false;
   static constexpr int kPer = 4;
+  // the largest of a vector, NaN if it holds one
+  static __device__ float largest(const uint4& v) {
+    return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)),
+                   max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
+  static __device__ uint4 finite(const uint4& v) { return v; }
   static constexpr uint32_t kNegInf = 0xFF800000u;
   static __device__ void unpack(const uint4& v, float (&f)[4]) {
     f[0] = __uint_as_float(v.x);
@@ -57,7 +75,26 @@ struct Logit<float> {
 };
 template <>
 struct Logit<__nv_bfloat16> {
+  static constexpr bool kPacked = true;
   static constexpr int kPer = 8;
+  static __device__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ float largest(const uint4& v) {
+    const uint32_t m = max2(max2(v.x, v.y), max2(v.z, v.w));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+  }
+  // -inf (and NaN) replaced by the lowest value
+  static __device__ uint4 finite(const uint4& v) {
+    uint4 r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r.x) : "r"(v.x), "r"(0xFF7FFF7Fu));
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r.y) : "r"(v.y), "r"(0xFF7FFF7Fu));
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r.z) : "r"(v.z), "r"(0xFF7FFF7Fu));
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r.w) : "r"(v.w), "r"(0xFF7FFF7Fu));
+    return r;
+  }
   static constexpr uint32_t kNegInf = 0xFF80FF80u;
   static __device__ void unpack(const uint4& v, float (&f)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -79,7 +116,19 @@ struct Logit<__nv_bfloat16> {
 };
 template <>
 struct Logit<__half> {
+  static constexpr bool kPacked = false;  // (its lowest value is an ordinary number)
   static constexpr int kPer = 8;
+  static __device__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ float largest(const uint4& v) {
+    const uint32_t m = max2(max2(v.x, v.y), max2(v.z, v.w));
+    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&m));
+    return max_nan(p.x, p.y);
+  }
+  static __device__ uint4 finite(const uint4& v) { return v; }
   static constexpr uint32_t kNegInf = 0xFC00FC00u;
   static __device__ void unpack(const uint4& v, float (&f)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -102,12 +151,6 @@ struct Logit<__half> {
 };
 
 // ------------------------------------------------------------- small pieces
-
-__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
 
 __device__ __forceinline__ float warp_max_nan(float v) {
   float r;
@@ -176,12 +219,30 @@ struct Row {
   __device__ uint4 load(int v) const {
     const int j0 = v * kPer - shift;
     if (inside(v)) return *reinterpret_cast<const uint4*>(z + j0);
-    uint4 raw = make_uint4(Logit<T>::kNegInf, Logit<T>::kNegInf, Logit<T>::kNegInf,
-                           Logit<T>::kNegInf);
+    uint4 raw = nothing();
     T* e = reinterpret_cast<T*>(&raw);
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
       if (j0 + i >= 0 && j0 + i < V) e[i] = z[j0 + i];
+    return raw;
+  }
+  static __device__ uint4 nothing() {
+    return make_uint4(Logit<T>::kNegInf, Logit<T>::kNegInf, Logit<T>::kNegInf,
+                      Logit<T>::kNegInf);
+  }
+  // `raw` with -inf at the places whose bit is 0.
+  static __device__ uint4 masked(uint4 raw, uint32_t b) {
+    uint32_t* w = reinterpret_cast<uint32_t*>(&raw);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t m;
+      if (kPer == 4) {
+        m = 0u - (b >> i & 1u);
+      } else {
+        m = (b >> (2 * i) & 1u ? 0xFFFFu : 0u) | (b >> (2 * i + 1) & 1u ? 0xFFFF0000u : 0u);
+      }
+      w[i] = (w[i] & m) | (Logit<T>::kNegInf & ~m);
+    }
     return raw;
   }
   // Bits of the allowed places of vector v (others of its bits are arbitrary).
@@ -272,14 +333,66 @@ __device__ void rank_keys(const unsigned long long* cand, int n, int k,
 }
 
 struct TopShared {
+  unsigned long long cand[kMaxCand];
+  unsigned long long list[kTopMax];
+  uint32_t group[kMaxWarps * 32];
+  int listed[kMaxListed];
   int chunk[kTopMax];
   int vec[kTopMax];
   uint32_t vkey[kTopMax * 32];
-  unsigned long long cand[kTopMax * 8];
-  unsigned long long list[kTopMax];
   uint32_t least;
-  int n_cand;
+  int n_cand, n_listed;
 };
+static_assert(kMaxCand >= kTopMax * 8 && kMaxCand >= kMaxCluster * kTopMax, "candidates fit");
+
+// Lanes a group: a power of two that leaves four groups an alternative, if the block has
+// as many lanes.
+__device__ __forceinline__ int bound_lanes(int k, int warps) {
+  int lanes = 32;
+  while (lanes > 1 && warps * 32 / lanes < 4 * k) lanes >>= 1;
+  return lanes;
+}
+
+// The candidates through the first k chunks and the first k vectors, whatever the ties
+// (the head of this file).  The whole block calls it; ckey: the maxima of its n_c chunks.
+template <typename T, bool kAllowed>
+__device__ __noinline__ void exact_candidates(const Row<T>& row, const uint32_t* ckey, int c0,
+                                              int n_c, int n_vec, int k, TopShared& sh) {
+  constexpr int kPer = Logit<T>::kPer;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int k1 = min(k, n_c), k2 = min(k, k1 * 32);
+  if (warp == 0) select_first(ckey, n_c, k1, lane, sh.chunk);
+  __syncthreads();
+  for (int i = warp; i < k1; i += warps) {
+    const int v = (c0 + sh.chunk[i]) * 32 + lane;
+    float vm = -INFINITY;
+    if (v < n_vec) {
+      uint4 raw = row.load(v);
+      if (kAllowed) raw = Row<T>::masked(raw, row.bits(v));
+      vm = Logit<T>::largest(raw);
+    }
+    sh.vkey[i * 32 + lane] = order_key(vm);
+  }
+  if (threadIdx.x == 0) sh.n_cand = 0;
+  __syncthreads();
+  if (warp == 0) {
+    const uint32_t least = select_first(sh.vkey, k1 * 32, k2, lane, sh.vec);
+    // with fewer vectors than alternatives, every place of theirs is a candidate
+    if (lane == 0) sh.least = k2 == k ? max(least, kNoPlace + 1u) : kNoPlace + 1u;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < k2 * kPer; i += blockDim.x) {
+    const int at = sh.vec[i / kPer];
+    const int v = (c0 + sh.chunk[at >> 5]) * 32 + (at & 31);
+    const int j = v * kPer - row.shift + i % kPer;
+    if (j < 0 || j >= row.V || !row.allows(j)) continue;
+    const uint32_t key = order_key(Logit<T>::value(row.z[j]));
+    if (key >= sh.least)
+      sh.cand[atomicAdd(&sh.n_cand, 1)] =
+          static_cast<unsigned long long>(key) << 32 | (0xffffffffu - static_cast<uint32_t>(j));
+  }
+}
+
 struct NoShared {};
 
 template <typename T, bool kAllowed, bool kTop>
@@ -323,31 +436,30 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
   const int c0 = static_cast<int>(static_cast<int64_t>(n_chunks) * rank / C);
   const int c1 = static_cast<int>(static_cast<int64_t>(n_chunks) * (rank + 1) / C);
 
+  // A warp takes kUnroll chunks at a time and has the next ones in flight.
   Sums a{-INFINITY, 0.0f, 0.0f};
-  for (int c = c0 + warp * kUnroll; c < c1; c += warps * kUnroll) {
-    uint4 raw[kUnroll];
-    uint32_t bits[kUnroll];
+  uint4 next[kUnroll];
+  auto fetch = [&](int c) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int v = (c + u) * 32 + lane;
-      const bool on = c + u < c1 && v < n_vec;
-      raw[u] = make_uint4(Logit<T>::kNegInf, Logit<T>::kNegInf, Logit<T>::kNegInf,
-                          Logit<T>::kNegInf);
-      if (on) raw[u] = row.load(v);
-      if (kAllowed) bits[u] = on ? row.bits(v) : 0u;
+      next[u] = Row<T>::nothing();
+      if (c + u < c1 && v < n_vec) {
+        next[u] = row.load(v);
+        if (kAllowed) next[u] = Row<T>::masked(next[u], row.bits(v));
+      }
     }
-    float f[kUnroll][kPer];
+  };
+  fetch(c0 + warp * kUnroll);
+  for (int c = c0 + warp * kUnroll; c < c1; c += warps * kUnroll) {
+    uint4 raw[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) raw[u] = next[u];
+    fetch(c + warps * kUnroll);
     float m = a.m;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      Logit<T>::unpack(raw[u], f[u]);
-      if (kAllowed) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) f[u][i] = bits[u] >> i & 1u ? f[u][i] : -INFINITY;
-      }
-      float vm = f[u][0];
-#pragma unroll
-      for (int i = 1; i < kPer; ++i) vm = max_nan(vm, f[u][i]);
+      const float vm = Logit<T>::largest(raw[u]);
       m = max_nan(m, vm);
       if (kTop) {
         const float cm = warp_max_nan(vm);
@@ -357,14 +469,33 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     const float ref = m == -INFINITY ? 0.0f : m;
     a = raised(a, ref, p.k);
     a.m = m;
+    // Distances below the float's range become its lowest value, so that e d is 0.  With a
+    // maximum of ordinary size (bf16) it is enough that the logits are finite.
+    if (Logit<T>::kPacked && fabsf(ref) <= 1e30f) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+      for (int u = 0; u < kUnroll; ++u) {
+        float f[kPer];
+        Logit<T>::unpack(Logit<T>::finite(raw[u]), f);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const float d = fmaxf(f[u][i] - ref, -FLT_MAX);
-        const float e = ex2_approx(d * p.k);
-        a.s += e;
-        a.t = fmaf(e, d, a.t);
+        for (int i = 0; i < kPer; ++i) {
+          const float d = f[i] - ref;
+          const float e = ex2_approx(d * p.k);
+          a.s += e;
+          a.t = fmaf(e, d, a.t);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        float f[kPer];
+        Logit<T>::unpack(raw[u], f);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const float d = fmaxf(f[i] - ref, -FLT_MAX);
+          const float e = ex2_approx(d * p.k);
+          a.s += e;
+          a.t = fmaf(e, d, a.t);
+        }
       }
     }
   }
@@ -389,41 +520,61 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
 
   if constexpr (kTop) {
     const int n_c = c1 - c0;
-    const int k1 = min(p.top, n_c);
-    if (warp == 0) select_first(ckey, n_c, k1, lane, s_top.chunk);
-    if (threadIdx.x == 0) s_top.n_cand = 0;
+    // The bound: the k-th largest of the maxima of `groups` groups of lanes.  With four
+    // groups an alternative, about 1.15 k logits reach it in random order.
+    const int lanes = bound_lanes(p.top, warps);
+    float lm = a.m;
+    for (int x = 1; x < lanes; x <<= 1) lm = fmaxf(lm, __shfl_xor_sync(0xffffffffu, lm, x));
+    const int groups = warps * 32 / lanes;
+    if (lane % lanes == 0) s_top.group[(warp * 32 + lane) / lanes] = order_key(lm);
+    if (threadIdx.x == 0) {
+      s_top.least = kNoPlace + 1u;  // with fewer groups than alternatives, every place
+      s_top.n_cand = 0;
+      s_top.n_listed = 0;
+    }
     __syncthreads();
-    for (int i = warp; i < k1; i += warps) {
-      const int v = (c0 + s_top.chunk[i]) * 32 + lane;
-      float vm = -INFINITY;
-      if (v < n_vec) {
-        float f[kPer];
-        Logit<T>::unpack(row.load(v), f);
-        const uint32_t b = kAllowed ? row.bits(v) : 0xffffffffu;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) vm = fmaxf(vm, b >> e & 1u ? f[e] : -INFINITY);
+    if (threadIdx.x < groups && p.top <= groups) {
+      const uint32_t mine = s_top.group[threadIdx.x];
+      int before = 0;
+      for (int g = 0; g < groups; ++g) {
+        const uint32_t other = s_top.group[g];
+        before += other > mine || (other == mine && g < static_cast<int>(threadIdx.x));
       }
-      s_top.vkey[i * 32 + lane] = order_key(vm);
+      if (before == p.top - 1) s_top.least = max(mine, kNoPlace + 1u);
     }
     __syncthreads();
-    const int k2 = min(p.top, k1 * 32);
-    if (warp == 0) {
-      const uint32_t least = select_first(s_top.vkey, k1 * 32, k2, lane, s_top.vec);
-      // with fewer vectors than alternatives, every place of theirs is a candidate
-      if (lane == 0) s_top.least = k2 == p.top ? max(least, kNoPlace + 1u) : kNoPlace + 1u;
+    const uint32_t least = s_top.least;
+    for (int i = threadIdx.x; i < n_c; i += blockDim.x)
+      if (ckey[i] >= least) {
+        const int at = atomicAdd(&s_top.n_listed, 1);
+        if (at < kMaxListed) s_top.listed[at] = i;
+      }
+    __syncthreads();
+    const int n_listed = s_top.n_listed;
+    if (n_listed <= kMaxListed) {
+      for (int i = warp; i < n_listed; i += warps) {
+        const int v = (c0 + s_top.listed[i]) * 32 + lane;
+        if (v >= n_vec) continue;
+        float f[kPer];
+        uint4 raw = row.load(v);
+        if (kAllowed) raw = Row<T>::masked(raw, row.bits(v));
+        Logit<T>::unpack(raw, f);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          const uint32_t key = order_key(f[e]);
+          if (key < least) continue;
+          const uint32_t j = static_cast<uint32_t>(v * kPer - row.shift + e);
+          const int at = atomicAdd(&s_top.n_cand, 1);
+          if (at < kMaxCand)
+            s_top.cand[at] = static_cast<unsigned long long>(key) << 32 | (0xffffffffu - j);
+        }
+      }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < k2 * kPer; i += blockDim.x) {
-      const int at = s_top.vec[i / kPer];
-      const int v = (c0 + s_top.chunk[at >> 5]) * 32 + (at & 31);
-      const int j = v * kPer - row.shift + i % kPer;
-      if (j < 0 || j >= row.V || !row.allows(j)) continue;
-      const uint32_t key = order_key(Logit<T>::value(row.z[j]));
-      if (key >= s_top.least)
-        s_top.cand[atomicAdd(&s_top.n_cand, 1)] =
-            static_cast<unsigned long long>(key) << 32 | (0xffffffffu - static_cast<uint32_t>(j));
+    if (n_listed > kMaxListed || s_top.n_cand > kMaxCand) {
+      exact_candidates<T, kAllowed>(row, ckey, c0, n_c, n_vec, p.top, s_top);
+      __syncthreads();
     }
-    __syncthreads();
     rank_keys(s_top.cand, s_top.n_cand, p.top, s_top.list);
   } else {
     __syncthreads();
