@@ -5,7 +5,10 @@
 //   S = sum e^((z - m) / t),   T = sum e^((z - m) / t) (z - m)
 //   lp = (z_y - m) / t - ln S,   H = ln S - T / (t S)
 // Both terms of H are >= 0, so a peaked row loses nothing to cancellation.  One pass: a
-// lane keeps (m, S, T) over its logits and rescales them when its maximum grows.
+// lane keeps (m, S, T) over its logits and rescales them when its maximum grows.  A bf16
+// logit takes some seven instructions (unpacking, bound, fused multiply-add, exponential,
+// two sums, a share of the packed maximum) of the eleven an SM can issue in the time its two
+// bytes take from memory.
 //
 // Alternatives without a second pass: the row is cut into chunks of 32 vectors of 16
 // bytes (one load of a warp), whose maxima the pass has at hand.  The k-th largest of the
@@ -58,7 +61,14 @@ struct Logit<float> {
     return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)),
                    max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
   }
-  static __device__ uint4 finite(const uint4& v) { return v; }
+  static __device__ uint4 finite(const uint4& v, uint32_t) { return v; }
+  template <int kN>
+  static __device__ float largest_of(const uint4 (&v)[kN]) {
+    float m = largest(v[0]);
+#pragma unroll
+    for (int i = 1; i < kN; ++i) m = max_nan(m, largest(v[i]));
+    return m;
+  }
   static constexpr uint32_t kNegInf = 0xFF800000u;
   static __device__ void unpack(const uint4& v, float (&f)[4]) {
     f[0] = __uint_as_float(v.x);
@@ -86,14 +96,23 @@ struct Logit<__nv_bfloat16> {
     const uint32_t m = max2(max2(v.x, v.y), max2(v.z, v.w));
     return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
   }
-  // -inf (and NaN) replaced by the lowest value
-  static __device__ uint4 finite(const uint4& v) {
-    uint4 r;
-    asm("max.bf16x2 %0, %1, %2;" : "=r"(r.x) : "r"(v.x), "r"(0xFF7FFF7Fu));
-    asm("max.bf16x2 %0, %1, %2;" : "=r"(r.y) : "r"(v.y), "r"(0xFF7FFF7Fu));
-    asm("max.bf16x2 %0, %1, %2;" : "=r"(r.z) : "r"(v.z), "r"(0xFF7FFF7Fu));
-    asm("max.bf16x2 %0, %1, %2;" : "=r"(r.w) : "r"(v.w), "r"(0xFF7FFF7Fu));
+  template <int kN>
+  static __device__ float largest_of(const uint4 (&v)[kN]) {
+    uint4 m = v[0];
+#pragma unroll
+    for (int i = 1; i < kN; ++i)
+      m = make_uint4(max2(m.x, v[i].x), max2(m.y, v[i].y), max2(m.z, v[i].z), max2(m.w, v[i].w));
+    return largest(m);
+  }
+  // at least the value in both halves of `low` (and no NaN)
+  static __device__ uint32_t bounded(uint32_t w, uint32_t low) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(low));
     return r;
+  }
+  static __device__ uint4 finite(const uint4& v, uint32_t low) {
+    return make_uint4(bounded(v.x, low), bounded(v.y, low), bounded(v.z, low),
+                      bounded(v.w, low));
   }
   static constexpr uint32_t kNegInf = 0xFF80FF80u;
   static __device__ void unpack(const uint4& v, float (&f)[8]) {
@@ -128,7 +147,14 @@ struct Logit<__half> {
     const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&m));
     return max_nan(p.x, p.y);
   }
-  static __device__ uint4 finite(const uint4& v) { return v; }
+  static __device__ uint4 finite(const uint4& v, uint32_t) { return v; }
+  template <int kN>
+  static __device__ float largest_of(const uint4 (&v)[kN]) {
+    float m = largest(v[0]);
+#pragma unroll
+    for (int i = 1; i < kN; ++i) m = max_nan(m, largest(v[i]));
+    return m;
+  }
   static constexpr uint32_t kNegInf = 0xFC00FC00u;
   static __device__ void unpack(const uint4& v, float (&f)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -173,28 +199,48 @@ __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
 
-__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-  return v;
-}
-__device__ __forceinline__ unsigned long long ld_cluster_u64(uint32_t a) {
-  unsigned long long v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
-  return v;
+__device__ __forceinline__ void st_cluster_u64(uint32_t a, unsigned long long v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
 }
 
-// The softmax sums of some of a row's logits (above); S = 0 without any.
+// The cluster barrier in two halves.
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// The softmax sums of some of a row's logits: m the largest, s = sum 2^d and t = sum 2^d d,
+// d = z k - c the distance to c, k = log2(e) / t, in powers of two.  c is m k rounded, so
+// that d is one fused multiply-add; it cancels everywhere but in ln S (log_sum).  Where
+// |m k| is over kOrdinary, c is m k itself and d is (z - m) k: the rounding of c could be
+// large there, or m k infinite.  s = 0 without any logits.
 struct Sums {
   float m, s, t;
 };
+constexpr float kOrdinary = 4096.0f;
+__device__ __forceinline__ bool ordinary(float c) { return fabsf(c) <= kOrdinary; }
+// m k - c
+__device__ __forceinline__ float shift_of(float m, float k) {
+  const float c = m * k;
+  return ordinary(c) ? fmaf(m, k, -c) : 0.0f;
+}
 
 // What `a` becomes when its maximum is raised to `m` (finite).
 __device__ __forceinline__ Sums raised(const Sums& a, float m, float k) {
-  const float d = fmaxf(a.m - m, -FLT_MAX);  // (a.m may be -inf)
-  const float f = ex2_approx(d * k);
+  const float c0 = a.m * k, c1 = m * k;
+  float d = c0 - c1;
+  if (!ordinary(c0) || !ordinary(c1))
+    d = fmaxf((a.m - m) * k - shift_of(a.m, k) + shift_of(m, k), -FLT_MAX);  // (a.m may be -inf)
+  const float f = ex2_approx(d);
   // f = 0: nothing is left, and d s may be infinite
   return {m, a.s * f, f > 0.0f ? f * fmaf(d, a.s, a.t) : 0.0f};
+}
+
+// ln sum e^((z - m) / t)
+__device__ __forceinline__ float log_sum(const Sums& a, float k) {
+  return fmaf(-0.69314718f, shift_of(a.m, k), logf(a.s));
 }
 
 // One row: where it starts, and which of its places count.
@@ -265,6 +311,7 @@ struct ForwardArgs {
   const int32_t* targets;
   float k;      // log2(e) / t
   float inv_t;
+  uint32_t low;  // twice a bf16 value that k times is finite and far below kOrdinary
   int top;
   int cluster;  // CTAs a row
   float *logprob, *entropy, *lse, *stats, *top_logprob;
@@ -332,18 +379,48 @@ __device__ void rank_keys(const unsigned long long* cand, int n, int k,
   __syncthreads();
 }
 
+// The k first of C lists of k keys (largest first, zeros where there are fewer).  A key's
+// place is the number of keys before it in every list, by bisection.
+__device__ void merge_lists(const unsigned long long* lists, int C, int k,
+                            unsigned long long* list) {
+  for (int i = threadIdx.x; i < k; i += blockDim.x) list[i] = 0ull;
+  __syncthreads();
+  for (int i = threadIdx.x; i < C * k; i += blockDim.x) {
+    const unsigned long long key = lists[i];
+    if (key == 0ull) continue;
+    int lo[kMaxCluster];
+#pragma unroll
+    for (int c = 0; c < kMaxCluster; ++c) lo[c] = 0;
+    for (int step = kTopMax / 2; step > 0; step >>= 1) {
+#pragma unroll
+      for (int c = 0; c < kMaxCluster; ++c)  // (the lists' searches overlap)
+        if (c < C && lo[c] + step <= k && lists[c * k + lo[c] + step - 1] > key) lo[c] += step;
+    }
+    int before = 0;
+#pragma unroll
+    for (int c = 0; c < kMaxCluster; ++c) {
+      if (c < C && lo[c] < k && lists[c * k + lo[c]] > key) ++lo[c];
+      before += lo[c];
+    }
+    if (before < k) list[before] = key;
+  }
+  __syncthreads();
+}
+
 struct TopShared {
-  unsigned long long cand[kMaxCand];
+  union {
+    unsigned long long cand[kMaxCand];
+    uint32_t vkey[kTopMax * 32];  // exact_candidates, until it has its vectors
+  };
   unsigned long long list[kTopMax];
-  uint32_t group[kMaxWarps * 32];
+  alignas(16) uint32_t group[kMaxWarps * 32];
   int listed[kMaxListed];
   int chunk[kTopMax];
   int vec[kTopMax];
-  uint32_t vkey[kTopMax * 32];
   uint32_t least;
   int n_cand, n_listed;
 };
-static_assert(kMaxCand >= kTopMax * 8 && kMaxCand >= kMaxCluster * kTopMax, "candidates fit");
+static_assert(kMaxCand >= kTopMax * 8, "candidates of the exact way fit");
 
 // Lanes a group: a power of two that leaves four groups an alternative, if the block has
 // as many lanes.
@@ -399,9 +476,14 @@ template <typename T, bool kAllowed, bool kTop>
 __global__ void __launch_bounds__(kMaxWarps * 32)
     logits_logprob_kernel(const ForwardArgs p) {
   constexpr int kPer = Logit<T>::kPer;
-  extern __shared__ uint32_t ckey[];  // kTop: the maxima of this CTA's chunks, as keys
+  // kTop: with several CTAs rank 0's copy of their lists; the maxima of this CTA's chunks,
+  // as keys
+  extern __shared__ __align__(8) unsigned char dyn[];
+  unsigned long long* const lists = reinterpret_cast<unsigned long long*>(dyn);
+  uint32_t* const ckey = reinterpret_cast<uint32_t*>(dyn + (p.cluster > 1 ? p.cluster * p.top * 8 : 0));
   __shared__ Sums s_warp[kMaxWarps];
-  __shared__ Sums s_cta, s_row;
+  __shared__ Sums s_cta[kMaxCluster];  // rank 0's: every CTA's
+  __shared__ Sums s_row;
   __shared__ typename std::conditional<kTop, TopShared, NoShared>::type s_top;
   const int C = p.cluster;
   const int64_t r = blockIdx.x / C;
@@ -422,6 +504,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     }
     return;
   }
+  if (C > 1) cluster_arrive();  // this CTA runs: its shared memory may be written
   const Row<T> row(p.lg, r);
   // the target's logit is on its way while the row is read
   int32_t y = 0;
@@ -436,10 +519,23 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
   const int c0 = static_cast<int>(static_cast<int64_t>(n_chunks) * rank / C);
   const int c1 = static_cast<int>(static_cast<int64_t>(n_chunks) * (rank + 1) / C);
 
-  // A warp takes kUnroll chunks at a time and has the next ones in flight.
+  // A warp takes kUnroll chunks at a time and has the next ones in flight.  Chunks all of
+  // whose vectors are whole, [f0, f1), are read without tests.
   Sums a{-INFINITY, 0.0f, 0.0f};
+  const int f0 = row.shift ? 1 : 0, f1 = (row.shift + row.V) / kPer / 32;
+  const uint4* const vectors = reinterpret_cast<const uint4*>(row.z - row.shift);
   uint4 next[kUnroll];
   auto fetch = [&](int c) {
+    if (c >= f0 && c + kUnroll <= min(f1, c1)) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) next[u] = vectors[(c + u) * 32 + lane];
+      if (kAllowed) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          next[u] = Row<T>::masked(next[u], row.bits((c + u) * 32 + lane));
+      }
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int v = (c + u) * 32 + lane;
@@ -455,31 +551,34 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     uint4 raw[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) raw[u] = next[u];
-    fetch(c + warps * kUnroll);
+    if (c + warps * kUnroll < c1) fetch(c + warps * kUnroll);
     float m = a.m;
+    if (kTop) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const float vm = Logit<T>::largest(raw[u]);
-      m = max_nan(m, vm);
-      if (kTop) {
+      for (int u = 0; u < kUnroll; ++u) {
+        const float vm = Logit<T>::largest(raw[u]);
+        m = max_nan(m, vm);
         const float cm = warp_max_nan(vm);
         if (lane == 0 && c + u < c1) ckey[c + u - c0] = order_key(cm);
       }
+    } else {
+      m = max_nan(m, Logit<T>::template largest_of<kUnroll>(raw));
     }
     const float ref = m == -INFINITY ? 0.0f : m;
-    a = raised(a, ref, p.k);
+    if (ref != a.m) a = raised(a, ref, p.k);
     a.m = m;
-    // Distances below the float's range become its lowest value, so that e d is 0.  With a
-    // maximum of ordinary size (bf16) it is enough that the logits are finite.
-    if (Logit<T>::kPacked && fabsf(ref) <= 1e30f) {
+    const float c_ref = ref * p.k;
+    if (ordinary(c_ref)) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         float f[kPer];
-        Logit<T>::unpack(Logit<T>::finite(raw[u]), f);
+        Logit<T>::unpack(Logit<T>::finite(raw[u], p.low), f);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          const float d = f[i] - ref;
-          const float e = ex2_approx(d * p.k);
+          // e d is 0 where e is: by the bound on bf16 logits, or here
+          float d = fmaf(f[i], p.k, -c_ref);
+          if (!Logit<T>::kPacked) d = fmaxf(d, -FLT_MAX);
+          const float e = ex2_approx(d);
           a.s += e;
           a.t = fmaf(e, d, a.t);
         }
@@ -491,8 +590,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
         Logit<T>::unpack(raw[u], f);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          const float d = fmaxf(f[i] - ref, -FLT_MAX);
-          const float e = ex2_approx(d * p.k);
+          const float d = fmaxf((f[i] - ref) * p.k, -FLT_MAX);
+          const float e = ex2_approx(d);
           a.s += e;
           a.t = fmaf(e, d, a.t);
         }
@@ -512,10 +611,19 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
   __syncthreads();
   if (warp == 0) {
     const Sums c = merge(lane < warps ? s_warp[lane] : none);
+    if (C > 1) cluster_wait();
     if (lane == 0) {
-      s_cta = c;
-      if (C == 1) s_row = c;
+      if (C == 1) {
+        s_row = c;
+      } else {  // to rank 0
+        const uint32_t at = cluster_addr(&s_cta[rank], 0);
+        st_cluster_u32(at, __float_as_uint(c.m));
+        st_cluster_u32(at + 4, __float_as_uint(c.s));
+        st_cluster_u32(at + 8, __float_as_uint(c.t));
+      }
     }
+  } else if (C > 1) {
+    cluster_wait();
   }
 
   if constexpr (kTop) {
@@ -536,9 +644,14 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     if (threadIdx.x < groups && p.top <= groups) {
       const uint32_t mine = s_top.group[threadIdx.x];
       int before = 0;
-      for (int g = 0; g < groups; ++g) {
-        const uint32_t other = s_top.group[g];
-        before += other > mine || (other == mine && g < static_cast<int>(threadIdx.x));
+      const int me = static_cast<int>(threadIdx.x);
+#pragma unroll 4
+      for (int g = 0; g < groups; g += 4) {
+        const uint4 o = *reinterpret_cast<const uint4*>(&s_top.group[g]);
+        before += (o.x > mine || (o.x == mine && g < me)) +
+                  (o.y > mine || (o.y == mine && g + 1 < me)) +
+                  (o.z > mine || (o.z == mine && g + 2 < me)) +
+                  (o.w > mine || (o.w == mine && g + 3 < me));
       }
       if (before == p.top - 1) s_top.least = max(mine, kNoPlace + 1u);
     }
@@ -552,21 +665,33 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     __syncthreads();
     const int n_listed = s_top.n_listed;
     if (n_listed <= kMaxListed) {
-      for (int i = warp; i < n_listed; i += warps) {
-        const int v = (c0 + s_top.listed[i]) * 32 + lane;
-        if (v >= n_vec) continue;
-        float f[kPer];
-        uint4 raw = row.load(v);
-        if (kAllowed) raw = Row<T>::masked(raw, row.bits(v));
-        Logit<T>::unpack(raw, f);
+      for (int i0 = warp; i0 < n_listed; i0 += warps * kUnroll) {  // kUnroll loads in flight
+        uint4 raw[kUnroll];
+        int v[kUnroll];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-          const uint32_t key = order_key(f[e]);
-          if (key < least) continue;
-          const uint32_t j = static_cast<uint32_t>(v * kPer - row.shift + e);
-          const int at = atomicAdd(&s_top.n_cand, 1);
-          if (at < kMaxCand)
-            s_top.cand[at] = static_cast<unsigned long long>(key) << 32 | (0xffffffffu - j);
+        for (int u = 0; u < kUnroll; ++u) {
+          const int i = i0 + u * warps;
+          v[u] = i < n_listed ? (c0 + s_top.listed[i]) * 32 + lane : n_vec;
+          raw[u] = Row<T>::nothing();
+          if (v[u] < n_vec) {
+            raw[u] = row.load(v[u]);
+            if (kAllowed) raw[u] = Row<T>::masked(raw[u], row.bits(v[u]));
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          if (order_key(Logit<T>::largest(raw[u])) < least) continue;
+          float f[kPer];
+          Logit<T>::unpack(raw[u], f);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) {
+            const uint32_t key = order_key(f[e]);
+            if (key < least) continue;
+            const uint32_t j = static_cast<uint32_t>(v[u] * kPer - row.shift + e);
+            const int at = atomicAdd(&s_top.n_cand, 1);
+            if (at < kMaxCand)
+              s_top.cand[at] = static_cast<unsigned long long>(key) << 32 | (0xffffffffu - j);
+          }
         }
       }
     }
@@ -581,34 +706,29 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
   }
 
   if (C > 1) {
-    cluster_sync();  // every CTA's sums and list are in its shared memory
-    if (rank == 0) {
-      if (warp == 0) {
-        Sums x = none;
-        if (lane < C) {
-          const uint32_t at = cluster_addr(&s_cta, lane);
-          x.m = __uint_as_float(ld_cluster_u32(at));
-          x.s = __uint_as_float(ld_cluster_u32(at + 4));
-          x.t = __uint_as_float(ld_cluster_u32(at + 8));
-        }
-        const Sums c = merge(x);
-        if (lane == 0) s_row = c;
-      }
-      if constexpr (kTop) {
-        for (int i = threadIdx.x; i < C * p.top; i += blockDim.x)
-          s_top.cand[i] = ld_cluster_u64(cluster_addr(&s_top.list[i % p.top], i / p.top));
-      }
+    if constexpr (kTop) {  // the list to rank 0
+      for (int i = threadIdx.x; i < p.top; i += blockDim.x)
+        st_cluster_u64(cluster_addr(&lists[rank * p.top + i], 0), s_top.list[i]);
     }
-    cluster_sync();  // read: the other CTAs may leave
-    if (rank != 0) return;
-    if constexpr (kTop) rank_keys(s_top.cand, C * p.top, p.top, s_top.list);
+    __syncwarp();
+    cluster_arrive();
+    if (rank != 0) return;  // nobody reads this CTA's memory
+    cluster_wait();
+    if (warp == 0) {
+      const Sums c = merge(lane < C ? s_cta[lane] : none);
+      if (lane == 0) s_row = c;
+    }
+    if constexpr (kTop)
+      merge_lists(lists, C, p.top, s_top.list);
+    else
+      __syncthreads();
   }
 
   const Sums all = s_row;
   const bool empty = all.m == -INFINITY;
   const bool bad = !(all.m < INFINITY);  // NaN or +inf among the places
   const float nan = __int_as_float(0x7fc00000);
-  const float log_s = empty ? 0.0f : logf(all.s);
+  const float log_s = empty ? 0.0f : log_sum(all, p.k);
   if (threadIdx.x == 0) {
     if (bad) report(p.status, PACE_ERR_NAN_INPUT);
     if (p.logprob) {
@@ -619,7 +739,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     }
     if (p.lse) p.lse[r] = bad ? nan : (empty ? -INFINITY : fmaf(all.m, p.inv_t, log_s));
     if (p.entropy)
-      p.entropy[r] = bad ? nan : (empty ? 0.0f : log_s - all.t / all.s * p.inv_t);
+      p.entropy[r] = bad ? nan : (empty ? 0.0f : logf(all.s) - 0.69314718f * (all.t / all.s));
     if (p.stats)
       reinterpret_cast<float2*>(p.stats)[r] =
           bad ? make_float2(nan, nan) : make_float2(all.m, log_s);
@@ -762,8 +882,8 @@ pace_status check_temperature(float t) {
   return t > 0.0f && isfinite(t) && isfinite(kLog2e / t) ? PACE_OK : PACE_ERR_INVALID_ARG;
 }
 
-// CTAs (a cluster) and warps for each row.  A wave wants some eight warps on every
-// scheduler; below that the row is split, but not into slices of less than a warp's
+// CTAs (a cluster) and warps for each row.  An SM holds four CTAs of eight warps; rows
+// that fill one wave of them at most are split, but not into slices of less than a warp's
 // four chunks.  A CTA's chunk maxima take 4 bytes each of shared memory, so rows of
 // more than 8,192 chunks are split too.
 struct RowSplit {
@@ -773,7 +893,7 @@ RowSplit split_row(int64_t n_rows, int n_chunks) {
   RowSplit s{1, 1};
   while (s.warps < kMaxWarps && s.warps * kUnroll < n_chunks) s.warps *= 2;
   const int64_t want = static_cast<int64_t>(sm_count()) * 4;
-  while (s.cluster < kMaxCluster && n_rows * s.cluster < want &&
+  while (s.cluster < kMaxCluster && 2 * n_rows * s.cluster <= want &&
          2 * s.cluster * s.warps * kUnroll <= n_chunks)
     s.cluster *= 2;
   while (s.cluster < kMaxCluster && n_chunks > 8192 * s.cluster) s.cluster *= 2;
@@ -791,7 +911,10 @@ pace_status launch_forward(ForwardArgs a, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.lg.n_rows * s.cluster), 1, 1);
   cfg.blockDim = dim3(static_cast<unsigned>(s.warps) * 32, 1, 1);
-  cfg.dynamicSmemBytes = kTop ? static_cast<size_t>(n_chunks / s.cluster + 1) * 4 : 0;
+  cfg.dynamicSmemBytes = 0;
+  if (kTop)
+    cfg.dynamicSmemBytes = static_cast<size_t>(n_chunks / s.cluster + 1) * 4 +
+                           (s.cluster > 1 ? static_cast<size_t>(s.cluster) * a.top * 8 : 0);
   cfg.stream = st;
   if (cfg.dynamicSmemBytes > 32768)  // (float32 rows of more than 8.4M places)
     PACE_TRY_CUDA(cudaFuncSetAttribute(logits_logprob_kernel<T, kAllowed, kTop>,
@@ -861,6 +984,9 @@ extern "C" pace_status pace_logits_logprob(const PaceLogits* logits, const int32
   a.targets = targets;
   a.k = kLog2e / temperature;
   a.inv_t = 1.0f / temperature;
+  const int low_exponent = 119 - ilogbf(a.k) < 100 ? 119 - ilogbf(a.k) : 100;
+  a.low = 0x8000u | static_cast<uint32_t>(low_exponent + 127) << 7;
+  a.low |= a.low << 16;
   a.top = top_k;
   a.cluster = 1;
   a.logprob = logprob;

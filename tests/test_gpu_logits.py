@@ -429,3 +429,19 @@ def test_refusals_of_the_library_need_no_gpu_work():
     assert call(allowed=fake, allowed_stride=3) == pace.ERR_INVALID_ARG
     assert L.pace_logits_logprob(None, fake, 1.0, 0, fake, None, None, None, None, None, None,
                                  None) == pace.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("offset", [0.0, 2800.0, 2850.0, 2900.0, 50000.0])
+@pytest.mark.parametrize("t", [0.7, 1e-6, 1e4])
+def test_large_logits_and_odd_temperatures(dtype, offset, t):
+    """Rows whose logits times 1 / t pass every size at which the sums are taken another way,
+    some of whose places lie far below, in both directions and together."""
+    g = torch.Generator().manual_seed(int(offset))
+    z = torch.randn(6, 5003, generator=g) * min(2.0, 2.0 * t)
+    z[1] -= offset
+    z[2] += offset
+    z[3, ::2] -= offset
+    z[4, 7::300] += offset
+    z[5, 100:4000] = -INF
+    check_forward(z.to(dtype).to(DEV), t, 5)
