@@ -415,19 +415,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && leader) {
+    // The whole warp runs the loop and one lane issues: loop counters and descriptors are
+    // then the warp's and not a lane's, and an instruction takes its operands as they are
+    // (one lane running it alone took 0.31 us for a K step of four MMAs, whatever their N).
+    if (leader) {
+      const bool issue = elect_one();
       uint32_t it = 0, tc = 0;
       bool ok = true;
       for (int ph = 0; ph < n_phases && ok; ++ph) {
         const Phase f(p, maps, ph, n_clusters);
-        const uint32_t da = f.a_mn ? 2048 : 32, db = f.b_mn ? 2048 : 32;
+        const uint32_t da = (f.a_mn ? 2048u : 32u) >> 4, db = (f.b_mn ? 2048u : 32u) >> 4;
+        const uint64_t a0 = operand_desc(smem_u32(smem), f.a_mn);
+        const uint64_t b0 = operand_desc(smem_u32(smem) + kStageA, f.b_mn);
         for (int64_t t = cid; t < f.deal.items && ok; t += n_clusters) {
           const Item im = f.item(t);
           if (im.n0 >= f.cols) continue;
           const uint32_t idesc = idesc_f16(im.tn, f.a_mn, f.b_mn);
           const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
           ++tc;
-          if (!mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u, abort_flag)) {
+          if (!__all_sync(0xffffffffu, mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u,
+                                                                 abort_flag))) {
             ok = false;
             break;
           }
@@ -435,29 +442,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           const uint32_t d_tmem = tmem_base + acc * TM;
           for (int kb = 0; kb < f.nkb; ++kb, ++it) {
             const uint32_t s = it % STAGES, par = (it / STAGES) & 1u;
-            if (!mbar_wait_bounded(&full[s], par, abort_flag)) {
+            if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], par, abort_flag))) {
               ok = false;
               break;
             }
             tc_fence_after();
-            const uint32_t sa = smem_u32(smem + s * kStageBytes);
-            const uint32_t sb = sa + kStageA;
+            // (addresses are in units of 16 bytes and stay within their field)
+            const uint64_t a = a0 + s * (kStageBytes >> 4), b = b0 + s * (kStageBytes >> 4);
+            if (issue) {
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k)
-              tc_mma_f16_pair(d_tmem, operand_desc(sa + k * da, f.a_mn),
-                              operand_desc(sb + k * db, f.b_mn), idesc,
-                              (kb > 0 || k > 0) ? 1u : 0u);
-            tc_commit_pair(cluster_addr(&empty[s], 0));
-            tc_commit_pair(cluster_addr(&empty[s], 1));
+              for (int k = 0; k < BK / 16; ++k)
+                tc_mma_f16_pair(d_tmem, a + k * da, b + k * db, idesc,
+                                (kb > 0 || k > 0) ? 1u : 0u);
+              tc_commit_both(&empty[s]);
+            }
+            __syncwarp();
           }
           if (!ok) break;
-          tc_commit_pair(cluster_addr(&tmem_full[acc], 0));
-          tc_commit_pair(cluster_addr(&tmem_full[acc], 1));
+          if (issue) tc_commit_both(&tmem_full[acc]);
+          __syncwarp();
         }
       }
-      if (!ok) give_up();
-      tc_commit_pair(cluster_addr(mma_done, 0));
-      mbar_wait_bounded(mma_done, 0, nullptr);
+      if (!ok && lane == 0) give_up();
+      __syncwarp();
+      if (issue) {
+        tc_commit_pair(cluster_addr(mma_done, 0));
+        mbar_wait_bounded(mma_done, 0, nullptr);
+      }
+      __syncwarp();
     }
   } else {
     // Epilogue: warps w and w + 4 share a quarter of the lanes (32 rows) and take half of the
