@@ -89,7 +89,7 @@ pace_status encode_f32_2d(CUtensorMap* tm, const void* ptr, int64_t rows, int64_
 
 pace_status encode_f16_3d(CUtensorMap* tm, const void* ptr, int64_t batch, int64_t rows,
                           int64_t cols, int64_t ld, int64_t batch_stride, int box_inner,
-                          int box_outer, bool swizzle) {
+                          int box_outer) {
   auto enc = tensor_map_encoder();
   if (!enc) return PACE_ERR_CUDA;
   cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
@@ -100,7 +100,7 @@ pace_status encode_f16_3d(CUtensorMap* tm, const void* ptr, int64_t batch, int64
   cuuint32_t estr[3] = {1, 1, 1};
   CUresult r = enc(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(ptr), dims, strides,
                    box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                   swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? PACE_OK : PACE_ERR_UNSUPPORTED_SHAPE;
 }

@@ -22,8 +22,9 @@
 // each CTA issues TMA loads of its 128 A rows and its half of the B tile into a 4-stage
 // ring, warp 1 of the even CTA issues tcgen05.mma.cta_group::2 (M 256, N 256 or 128, K 16),
 // warps 2-9 of each CTA drain one of two accumulators while the next tile is computed.  A
-// and C are symmetric, so only tiles on and below the diagonal are computed and each is
-// also stored transposed: 3 s^2 l + s^3 operations a step instead of 4 s^2 l + 2 s^3.
+// and C are symmetric, so only tiles on and below the diagonal are computed and stored, and
+// what a product needs from above it is read from below in the other major order: 3 s^2 l +
+// s^3 operations a step instead of 4 s^2 l + 2 s^3.
 // The last phase's epilogue holds the update itself: it is written out in bf16, or goes
 // straight into the weights.
 #include <cuda.h>
@@ -62,9 +63,8 @@ constexpr int kNormBlocks = 128;  // partial sums of a matrix's norm
 enum { kGram = 0, kPoly = 1, kStep = 2 };
 
 struct Maps {
-  // loads: K-major (64 x 128 and 64 x 64 boxes), MN-major (64 x 64)
-  CUtensorMap xk[2], xk64[2], xm[2], ak, ak64, ck, ck64;
-  CUtensorMap xs[2], as, cs, at, ct;  // stores: 32-row tiles, and transposed ones
+  CUtensorMap x128[2], x64[2], a128, a64, c128, c64;  // loads: boxes of 64 x 128 and 64 x 64
+  CUtensorMap xs[2], as, cs;                          // stores: 64 x 32
 };
 
 struct NsArgs {
@@ -147,6 +147,7 @@ struct Item {
   int z, i, j;
   int32_t n0, tn;
 };
+constexpr int kBlocksPerTile = TM / BK;
 
 struct Phase {
   int kind, cur;           // cur: which X is read
@@ -155,8 +156,10 @@ struct Phase {
   Deal deal;
   int nkb;                 // K steps
   int64_t cols;            // of the product
-  const CUtensorMap *ma, *mb, *mb64;
-  bool a_mn, b_mn;
+  // Operands.  X is read K-major or MN-major; of a symmetric matrix only the tiles on and
+  // below the diagonal are there, so its blocks above it are read from below, MN-major.
+  const CUtensorMap *ma128, *ma64, *mb128, *mb64;
+  bool a_sym, b_sym, a_mn, b_mn;
 
   __device__ Phase(const NsArgs& p, const Maps& m, int ph, int n_clusters) {
     kind = ph % 3;
@@ -171,23 +174,37 @@ struct Phase {
     deal = deal_tiles(static_cast<int64_t>(per) * p.batch, n_clusters);
     nkb = static_cast<int>(((kind == kGram ? p.l : p.s) + BK - 1) / BK);
     cols = sym || p.tall ? p.s : p.l;
-    a_mn = b_mn = false;
+    a_mn = b_mn = a_sym = b_sym = false;
     if (kind == kGram) {
-      ma = mb = p.tall ? &m.xm[cur] : &m.xk[cur];
-      mb64 = p.tall ? &m.xm[cur] : &m.xk64[cur];
+      ma128 = mb128 = &m.x128[cur];
+      ma64 = mb64 = &m.x64[cur];
       a_mn = b_mn = p.tall;
     } else if (kind == kPoly) {
-      ma = mb = &m.ak;
-      mb64 = &m.ak64;
+      ma128 = mb128 = &m.a128;
+      ma64 = mb64 = &m.a64;
+      a_sym = b_sym = true;
     } else if (p.tall) {
-      ma = &m.xk[cur];
-      mb = &m.ck;
-      mb64 = &m.ck64;
+      ma128 = &m.x128[cur];
+      ma64 = &m.x64[cur];
+      mb128 = &m.c128;
+      mb64 = &m.c64;
+      b_sym = true;
     } else {
-      ma = &m.ck;
-      mb = mb64 = &m.xm[cur];
+      ma128 = &m.c128;
+      ma64 = &m.c64;
+      mb128 = &m.x128[cur];
+      mb64 = &m.x64[cur];
+      a_sym = true;
       b_mn = true;
     }
+  }
+
+  // Whether K block kb of an item's operand is read MN-major.
+  __device__ bool a_mn_at(const Item& it, int kb) const {
+    return a_sym ? kb / kBlocksPerTile > it.i : a_mn;
+  }
+  __device__ bool b_mn_at(const Item& it, int kb) const {
+    return b_sym ? kb / kBlocksPerTile > it.j : b_mn;
   }
 
   // CTAs that have items: only they write, and arrive at the barrier that ends the phase.
@@ -372,23 +389,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive(opened);
       }
       before += f.arrivals(n_clusters);
-      const int boxes_a = f.a_mn ? 2 : 1;
-      const bool is_a = lane < boxes_a;
-      const int box = is_a ? lane : lane - boxes_a;  // which 64-wide box of an MN-major tile
-      const bool mn = is_a ? f.a_mn : f.b_mn;
-      const uint32_t dst = (is_a ? 0u : kStageA) + box * 8192u;
       for (int64_t t = cid; t < f.deal.items && ok; t += n_clusters) {
         const Item im = f.item(t);
         if (im.n0 >= f.cols) continue;  // the second half of a narrow last tile
-        const int boxes = boxes_a + (f.b_mn ? im.tn / 128 : 1);
-        const CUtensorMap* desc = is_a ? f.ma : im.tn == TM ? f.mb : f.mb64;
-        const int32_t r0 = is_a ? im.i * TM + static_cast<int32_t>(crank) * BM
-                                : im.n0 + static_cast<int32_t>(crank) * (im.tn / 2);
-        const int32_t x = mn ? r0 + 64 * box : 0, dx = mn ? 0 : BK;
-        const int32_t y = mn ? 0 : r0, dy = mn ? BK : 0;
+        const int32_t ra = im.i * TM + static_cast<int32_t>(crank) * BM;
+        const int32_t rb = im.n0 + static_cast<int32_t>(crank) * (im.tn / 2);
         const uint32_t bytes = 2 * (kStageA + im.tn * BK);
         for (int kb = 0; kb < f.nkb; ++kb, ++it) {
           const uint32_t s = it % STAGES, par = (it / STAGES) & 1u;
+          // this lane's box: K-major 64 (K) x 128 or 64 rows; MN-major 64 x 64 (K), one or two
+          const bool a_mn = f.a_mn_at(im, kb), b_mn = f.b_mn_at(im, kb);
+          const int boxes_a = a_mn ? 2 : 1, boxes = boxes_a + (b_mn ? im.tn / 128 : 1);
+          const bool is_a = lane < boxes_a;
+          const int box = is_a ? lane : lane - boxes_a;
+          const bool mn = is_a ? a_mn : b_mn;
+          const int32_t r = (is_a ? ra : rb) + 64 * box, k = kb * BK;
+          const bool tall_box = !mn && (is_a || im.tn == TM);
+          const CUtensorMap* desc = is_a ? (tall_box ? f.ma128 : f.ma64)
+                                         : (tall_box ? f.mb128 : f.mb64);
           if (!__all_sync(0xffffffffu, mbar_wait_bounded(&empty[s], par ^ 1u, abort_flag))) {
             ok = false;
             break;
@@ -397,8 +415,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           if (leader && lane == 0) mbar_arrive_expect_tx(&full[s], bytes);
           __syncwarp();  // the lanes' loads are one TMA instruction
           if (lane < boxes)
-            tma_load_3d_pair(smem + s * kStageBytes + dst, desc, bar, x + kb * dx, y + kb * dy,
-                             im.z, pol);
+            tma_load_3d_pair(smem + s * kStageBytes + (is_a ? 0u : kStageA) + box * 8192u, desc,
+                             bar, mn ? r : k, mn ? k : r, im.z, pol);
         }
       }
     }
@@ -424,13 +442,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bool ok = true;
       for (int ph = 0; ph < n_phases && ok; ++ph) {
         const Phase f(p, maps, ph, n_clusters);
-        const uint32_t da = (f.a_mn ? 2048u : 32u) >> 4, db = (f.b_mn ? 2048u : 32u) >> 4;
-        const uint64_t a0 = operand_desc(smem_u32(smem), f.a_mn);
-        const uint64_t b0 = operand_desc(smem_u32(smem) + kStageA, f.b_mn);
         for (int64_t t = cid; t < f.deal.items && ok; t += n_clusters) {
           const Item im = f.item(t);
           if (im.n0 >= f.cols) continue;
-          const uint32_t idesc = idesc_f16(im.tn, f.a_mn, f.b_mn);
           const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
           ++tc;
           if (!__all_sync(0xffffffffu, mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u,
@@ -448,7 +462,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
             tc_fence_after();
             // (addresses are in units of 16 bytes and stay within their field)
-            const uint64_t a = a0 + s * (kStageBytes >> 4), b = b0 + s * (kStageBytes >> 4);
+            const bool a_mn = f.a_mn_at(im, kb), b_mn = f.b_mn_at(im, kb);
+            const uint32_t idesc = idesc_f16(im.tn, a_mn, b_mn);
+            const uint32_t da = (a_mn ? 2048u : 32u) >> 4, db = (b_mn ? 2048u : 32u) >> 4;
+            const uint32_t at = smem_u32(smem) + s * kStageBytes;
+            const uint64_t a = operand_desc(at, a_mn), b = operand_desc(at + kStageA, b_mn);
             if (issue) {
 #pragma unroll
               for (int k = 0; k < BK / 16; ++k)
@@ -493,7 +511,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       const int64_t rows = f.sym ? p.s : p.x_rows;
       const CUtensorMap* store =
           f.kind == kGram ? &maps.as : f.kind == kPoly ? &maps.cs : &maps.xs[f.cur ^ 1];
-      const CUtensorMap* mirror = f.kind == kGram ? &maps.at : &maps.ct;
       // value = f_acc * accumulator (+ f_src * A + diag on the diagonal)
       float f_acc, f_src = 0.0f, diag = 0.0f;
       if (f.kind == kGram) {
@@ -542,16 +559,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             if (row_w >= rows || col0 >= f.cols) break;
             if (f.kind == kPoly && c0 != c_begin) load_a(c0);
             // 32 rows x 64 columns leave as one TMA tile of 128-byte rows (128-byte
-            // swizzle: the lanes' 16-byte stores are conflict-free), and transposed as 64
-            // rows of 32
-            const bool flip = f.sym && im.i != im.j;
-            if (lane == 0) {
-              if (f.sym) bulk_wait_read<0>();
-              else bulk_wait_read<1>();
-            }
+            // swizzle: the lanes' 16-byte stores are conflict-free), two in turn
+            if (lane == 0) bulk_wait_read<1>();
             __syncwarp();
-            unsigned char* tile = stage + (flip ? 0u : (n_out++ & 1u) * kOutTile);
-            uint16_t* tcol = reinterpret_cast<uint16_t*>(stage + kOutTile) + lane;
+            unsigned char* tile = stage + (n_out++ & 1u) * kOutTile;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               float v[32];
@@ -584,22 +595,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               for (int q = 0; q < 4; ++q)
                 *reinterpret_cast<uint4*>(tile + lane * 128 + (((4 * k + q) ^ (lane & 7)) << 4)) =
                     make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
-              if (flip) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  tcol[(32 * k + 2 * i) * 32] = static_cast<uint16_t>(h[i] & 0xffffu);
-                  tcol[(32 * k + 2 * i + 1) * 32] = static_cast<uint16_t>(h[i] >> 16);
-                }
-              }
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
               tma_store_3d(store, tile, static_cast<int32_t>(col0), static_cast<int32_t>(row_w),
                            im.z);
-              if (flip)
-                tma_store_3d(mirror, stage + kOutTile, static_cast<int32_t>(row_w),
-                             static_cast<int32_t>(col0), im.z);
               bulk_commit();
             }
           }
@@ -641,7 +642,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
       if (warp == 2 && lane == 0 && !*abort_flag) {
-        __threadfence();
         red_release(p.ctr);
       }
     }
@@ -942,22 +942,19 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
   Maps m;
   const int64_t xbs = u.rows * w.ldx, cbs = n.s * w.lda;
   for (int i = 0; i < 2; ++i) {
-    PACE_TRY(encode_f16_3d(&m.xk[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 128, true));
-    PACE_TRY(encode_f16_3d(&m.xk64[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 64, true));
-    PACE_TRY(encode_f16_3d(&m.xs[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 32, true));
-    m.xm[i] = m.xk64[i];
+    PACE_TRY(encode_f16_3d(&m.x128[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 128));
+    PACE_TRY(encode_f16_3d(&m.x64[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 64));
+    PACE_TRY(encode_f16_3d(&m.xs[i], w.x[i], batch, u.rows, u.cols, w.ldx, xbs, 64, 32));
   }
-  auto square = [&](CUtensorMap* tm, __half* at, int inner, int outer, bool swizzle) {
-    return encode_f16_3d(tm, at, batch, n.s, n.s, w.lda, cbs, inner, outer, swizzle);
+  auto square = [&](CUtensorMap* tm, __half* at, int outer) {
+    return encode_f16_3d(tm, at, batch, n.s, n.s, w.lda, cbs, 64, outer);
   };
-  PACE_TRY(square(&m.ak, w.a, 64, 128, true));
-  PACE_TRY(square(&m.ak64, w.a, 64, 64, true));
-  PACE_TRY(square(&m.as, w.a, 64, 32, true));
-  PACE_TRY(square(&m.at, w.a, 32, 64, false));
-  PACE_TRY(square(&m.ck, w.c, 64, 128, true));
-  PACE_TRY(square(&m.ck64, w.c, 64, 64, true));
-  PACE_TRY(square(&m.cs, w.c, 64, 32, true));
-  PACE_TRY(square(&m.ct, w.c, 32, 64, false));
+  PACE_TRY(square(&m.a128, w.a, 128));
+  PACE_TRY(square(&m.a64, w.a, 64));
+  PACE_TRY(square(&m.as, w.a, 32));
+  PACE_TRY(square(&m.c128, w.c, 128));
+  PACE_TRY(square(&m.c64, w.c, 64));
+  PACE_TRY(square(&m.cs, w.c, 32));
 
   int max_clusters = 0;
   PACE_TRY(ns_max_clusters(&max_clusters));

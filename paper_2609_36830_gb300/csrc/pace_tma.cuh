@@ -20,9 +20,9 @@ pace_status encode_f32_2d(CUtensorMap* tm, const void* ptr, int64_t rows, int64_
                           int box_inner, int box_outer);
 
 // fp16 matrices [batch][rows][cols] (strides in elements, multiples of 8), boxes of
-// box_inner x box_outer of one matrix, with the 128-byte swizzle or none.
+// box_inner x box_outer of one matrix, with the 128-byte swizzle.
 pace_status encode_f16_3d(CUtensorMap* tm, const void* ptr, int64_t batch, int64_t rows,
                           int64_t cols, int64_t ld, int64_t batch_stride, int box_inner,
-                          int box_outer, bool swizzle);
+                          int box_outer);
 
 }  // namespace pace
