@@ -529,7 +529,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         ++tc;
         const int64_t row_w = static_cast<int64_t>(im.i) * TM + crank * BM + quad * 32;
         const int64_t row = row_w + lane;
-        const int c_begin = side * (im.tn / 2), c_end = c_begin + im.tn / 2;
+        const int c_begin = side * (im.tn / 2);
         // A's entries (of 64 columns) are on their way while the product is computed
         uint4 src[8];
         const __half* a_row = p.a + (static_cast<int64_t>(im.z) * p.s + row) * p.lda + im.n0;
@@ -551,12 +551,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         tc_fence_after();
         const uint32_t tbase = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + acc * TM;
-        if (!f.last) {
+        // The accumulator is free once this warp's last columns are in registers.  (An
+        // arrival that releases at cluster scope waits for the stores and copies in
+        // flight, 1 us.)
+        const int64_t cols_left = f.cols - im.n0 - c_begin;
+        const int mine = row_w >= rows || cols_left <= 0 ? 0
+                         : cols_left < im.tn / 2 ? static_cast<int>(cols_left) : im.tn / 2;
+        auto release = [&]() {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_pair(acc ? empty1 : empty0);
+        };
+        if (mine == 0) {
+          release();
+        } else if (!f.last) {
 #pragma unroll 1
-          for (int c0 = c_begin; c0 < c_end; c0 += 64) {
+          for (int c0 = c_begin; c0 < c_begin + mine; c0 += 64) {
             const int64_t col0 = im.n0 + c0;
-            // the same for the warp; and later columns are outside too
-            if (row_w >= rows || col0 >= f.cols) break;
             if (f.kind == kPoly && c0 != c_begin) load_a(c0);
             // 32 rows x 64 columns leave as one TMA tile of 128-byte rows (128-byte
             // swizzle: the lanes' 16-byte stores are conflict-free), two in turn
@@ -568,6 +579,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               float v[32];
               tmem_ld_32x32b_x32(tbase + c0 + 32 * k, v);
               tmem_wait_ld();
+              if (k == 1 && c0 + 64 >= c_begin + mine) release();
 #pragma unroll
               for (int i = 0; i < 32; ++i) v[i] *= f_acc;
               if (f.kind == kPoly) {
@@ -610,14 +622,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           float* tile = reinterpret_cast<float*>(stage);
           Block b{row_w, rows, 0, f.cols, im.z};
 #pragma unroll 1
-          for (int c = c_begin; c < c_end; c += 32) {
+          for (int c = c_begin; c < c_begin + mine; c += 32) {
             b.col0 = im.n0 + c;
-            if (row_w >= rows || b.col0 >= f.cols) break;
             float4 w[8];
             if (p.vec && p.weight) load_weights(p, b, lane, w);
             float v[32];
             tmem_ld_32x32b_x32(tbase + c, v);
             tmem_wait_ld();
+            if (c + 32 >= c_begin + mine) release();
             __syncwarp();
 #pragma unroll
             for (int q = 0; q < 8; ++q)
@@ -631,9 +643,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
               store_result1(p, b, lane, tile);
           }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
       }
       // the CTA's tiles are in memory: one arrival for it, and the next phase may read them
       if (lane == 0) {

@@ -174,6 +174,12 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_caddr) {
                : "memory");
 }
 
+// The same with the default semantics, which do not wait for the thread's stores and
+// copies in flight.
+__device__ __forceinline__ void mbar_arrive_pair(uint32_t bar_caddr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar_caddr) : "memory");
+}
+
 // Arrive on the mbarrier at cluster address bar_caddr (this CTA's or a peer's)
 // and raise its expected transaction bytes by `bytes`, in one step.
 __device__ __forceinline__ void mbar_arrive_expect_tx_cluster(uint32_t bar_caddr, uint32_t bytes) {
