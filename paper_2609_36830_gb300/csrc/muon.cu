@@ -859,6 +859,279 @@ __global__ void __launch_bounds__(kElemThreads, 4) direction_kernel(const UArgs 
   }
 }
 
+// ------------------------------------------------------------- matrices up to 256 x 256
+
+// One CTA pair does everything for a matrix of at most 256 x 256, in shared memory and
+// without a grid barrier: norm, all products, result.  (The phases of
+// newton_schulz_kernel spend 4-5 us each in barrier, loads and stores whatever the size.)
+// X is s x l with s <= l, so a tall U is transposed as it is read.  Operands lie in the
+// layouts that the TMA would build (128-byte swizzle), 64 KB each in a CTA:
+//   rows     the CTA's 128 rows of X, and of C: [K block][128 rows][64], K-major.  They are
+//            the A operand and, because X X^T takes X twice and A and C are symmetric, its
+//            half of the B operand as well;
+//   gram     the same of A;
+//   columns  the CTA's 128 columns of X: [K block][64-column box][64 rows of X][64],
+//            MN-major, the B operand of C X.
+// C takes the place of the rows of X once X X^T is done; a step's result goes to the CTA's
+// own rows and to the columns of either CTA.
+constexpr int kSmallThreads = 32 * (kEpiWarps + 1);
+constexpr uint32_t kRegion = 65536;
+constexpr size_t kSmallSmem = 1024 + 3 * kRegion + 256;
+constexpr int kSmallSide = 256;
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
+    newton_schulz_small_kernel(const __grid_constant__ UArgs u, const __grid_constant__ NsArgs p) {
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  unsigned char* rows_at = smem;
+  unsigned char* gram_at = smem + kRegion;
+  unsigned char* cols_at = smem + 2 * kRegion;
+  uint64_t* done = reinterpret_cast<uint64_t*>(smem + 3 * kRegion);  // a product is complete
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* pair_sum = reinterpret_cast<float*>(tmem_slot + 2);   // [2] the CTAs' squares
+  float* warp_sum = pair_sum + 2;                              // [kEpiWarps]
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t crank = cluster_ctarank();
+  const int z = static_cast<int>(blockIdx.x) / 2;
+  const int s = static_cast<int>(p.s), l = static_cast<int>(p.l);
+  const int ks = (s + BK - 1) / BK, kl = (l + BK - 1) / BK;  // K blocks of either side
+
+  if (threadIdx.x == 0) {
+    mbar_init(done, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  cluster_sync();  // both CTAs run and their barriers exist
+  if (warp == kEpiWarps) {
+    tmem_alloc_pair(tmem_slot, TM);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  cluster_sync();  // both CTAs' tensor memory is allocated before any MMA writes it
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  // Thread of the epilogue: row of X, and 128 of its columns.
+  const int quad = warp & 3, side = warp >> 2;
+  const int row_l = quad * 32 + lane;
+  const int row = static_cast<int>(crank) * BM + row_l;
+  // U's values at 32 columns of the thread's row (zeros outside), momentum updated if kNorm
+  auto load_u = [&](int col0, bool update, float (&v)[32]) {
+    if (!p.tall && u.vec && row < s) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (col0 + 8 * q < l) {
+          if (update) direction8<true>(u, z, row, col0 + 8 * q, f);
+          else direction8<false>(u, z, row, col0 + 8 * q, f);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[8 * q + i] = f[i];
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const int col = col0 + i;
+      v[i] = 0.0f;
+      if (row >= s || col >= l) continue;
+      const int64_t ur = p.tall ? col : row, uc = p.tall ? row : col;
+      v[i] = load1(u, z * u.bs + ur * u.ld + uc);
+      if (u.momentum) {
+        float* mp = u.momentum + (z * u.rows + ur) * u.cols + uc;
+        float m = *mp;
+        if (update) *mp = m = fmaf(u.mu, m, v[i]);
+        v[i] = direction(u, v[i], m);
+      }
+    }
+  };
+  // 32 columns of a row in a K-major region
+  auto put_rows = [&](unsigned char* region, int col0, const uint32_t (&h)[16]) {
+    unsigned char* at = region + (col0 >> 6) * 16384 + row_l * 128;
+    const int q0 = (col0 & 63) >> 3;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<uint4*>(at + (((q0 + q) ^ (row_l & 7)) << 4)) =
+          make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+  };
+  // the same 32 columns of X for the B operand of C X, in the CTA that holds the columns
+  const uint32_t cols_peer = cluster_addr(cols_at, static_cast<uint32_t>(side));
+  auto put_columns = [&](int col0, const uint32_t (&h)[16]) {
+    const int n = col0 - side * BM;
+    const uint32_t at = cols_peer + (row >> 6) * 16384 + (n >> 6) * 8192 + (row & 63) * 128;
+    const int q0 = (n & 63) >> 3;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(
+                       at + (((q0 + q) ^ (row & 7)) << 4)),
+                   "r"(h[4 * q]), "r"(h[4 * q + 1]), "r"(h[4 * q + 2]), "r"(h[4 * q + 3])
+                   : "memory");
+  };
+
+  // The norm: squares of the thread, the warp, the CTA, the pair.
+  if (warp < kEpiWarps) {
+    float ss = 0.0f;
+#pragma unroll 1
+    for (int c = side * BM; c < side * BM + BM && c < l; c += 32) {
+      float v[32];
+      load_u(c, true, v);
+      float part = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) part = fmaf(v[i], v[i], part);
+      ss += part;
+    }
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, x);
+    if (lane == 0) warp_sum[warp] = ss;
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    float sum = 0.0f;
+    for (int w = 0; w < kEpiWarps; ++w) sum += warp_sum[w];
+    st_cluster_u32(cluster_addr(&pair_sum[crank], threadIdx.x), __float_as_uint(sum));
+  }
+  cluster_sync();
+  const float norm = sqrtf(pair_sum[0] + pair_sum[1]);
+  const float scale = p.sx / (norm + u.eps);
+  if (!(norm < INFINITY) && crank == 0 && threadIdx.x == 0) report(p.status, PACE_ERR_NAN_INPUT);
+  if (warp < kEpiWarps) {
+#pragma unroll 1
+    for (int c = side * BM; c < side * BM + BM && c < kl * BK; c += 32) {
+      float v[32];
+      load_u(c, false, v);
+      uint32_t h[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i] * scale, v[2 * i + 1] * scale);
+      put_rows(rows_at, c, h);
+      put_columns(c, h);
+    }
+  }
+
+  bool ok = true;
+  const int n_phases = 3 * p.steps;
+  for (int ph = 0; ph < n_phases; ++ph) {
+    const int kind = ph % 3;
+    const bool last = ph == n_phases - 1;
+    // the operands are written, in both CTAs, before the tensor cores read them
+    fence_proxy_async();
+    tc_fence_before();
+    cluster_sync();
+    tc_fence_after();
+    if (warp == kEpiWarps) {
+      if (crank == 0 && elect_one()) {
+        const uint32_t a_at = smem_u32(kind == kPoly ? gram_at : rows_at);
+        const uint32_t b_at = smem_u32(kind == kStep ? cols_at : kind == kPoly ? gram_at : rows_at);
+        const bool b_mn = kind == kStep;
+        const uint32_t idesc = idesc_f16(TM, false, b_mn);
+        const int nkb = kind == kGram ? kl : ks;
+        for (int kb = 0; kb < nkb; ++kb) {
+          const uint64_t a = operand_desc(a_at + kb * 16384, false);
+          const uint64_t b = operand_desc(b_at + kb * 16384, b_mn);
+#pragma unroll
+          for (int k = 0; k < BK / 16; ++k)
+            tc_mma_f16_pair(tmem, a + k * 2, b + k * (b_mn ? 128 : 2), idesc,
+                            (kb > 0 || k > 0) ? 1u : 0u);
+        }
+        tc_commit_both(done);
+      }
+      __syncwarp();
+      continue;
+    }
+    if (ok && !__all_sync(0xffffffffu, mbar_wait_bounded(done, ph & 1, abort_flag))) {
+      if (!*abort_flag) report(p.status, PACE_ERR_TIMEOUT);
+      *abort_flag = 1;
+      ok = false;
+    }
+    if (!ok) continue;  // the barriers go on
+    tc_fence_after();
+    const uint32_t tbase = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    float f_acc, f_src = 0.0f, diag = 0.0f;
+    if (kind == kGram) {
+      f_acc = p.sa / (p.sx * p.sx);
+    } else if (kind == kPoly) {
+      f_acc = p.cc * p.sc / (p.sa * p.sa);
+      f_src = p.cb * p.sc / p.sa;
+      diag = p.ca * p.sc;
+    } else {
+      f_acc = last ? 1.0f / (p.sc * p.sx) : 1.0f / p.sc;
+    }
+    const int width = last ? l : (kind == kStep ? kl : ks) * BK;
+#pragma unroll 1
+    for (int c = side * BM; c < side * BM + BM && c < width; c += 32) {
+      float v[32];
+      tmem_ld_32x32b_x32(tbase + c, v);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] *= f_acc;
+      if (!last) {
+        if (kind == kPoly) {
+          const unsigned char* at = gram_at + (c >> 6) * 16384 + row_l * 128;
+          const int q0 = (c & 63) >> 3;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint4 w4 =
+                *reinterpret_cast<const uint4*>(at + (((q0 + q) ^ (row_l & 7)) << 4));
+            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 x = half2_value(w[i]);
+              v[8 * q + 2 * i] = fmaf(x.x, f_src, v[8 * q + 2 * i]);
+              v[8 * q + 2 * i + 1] = fmaf(x.y, f_src, v[8 * q + 2 * i + 1]);
+            }
+          }
+          if (row - lane == c) {  // the diagonal passes through the warp's block
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (lane == i) v[i] += diag;
+          }
+        }
+        uint32_t h[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i], v[2 * i + 1]);
+        put_rows(kind == kGram ? gram_at : rows_at, c, h);
+        if (kind == kStep) put_columns(c, h);
+      } else if (p.tall) {  // rows of X are columns of the result: whole lines as they are
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          if (row >= s || c + i >= l) continue;
+          if (p.weight) {
+            const int64_t at = (static_cast<int64_t>(z) * l + c + i) * s + row;
+            const float w = fmaf(p.weight[at], p.keep, -p.rate * v[i]);
+            p.weight[at] = w;
+            if (p.weight16) p.weight16[at] = __float2bfloat16_rn(w);
+          } else {
+            p.out[z * p.out_bs + (c + i) * p.out_ld + row] = __float2bfloat16_rn(v[i]);
+          }
+        }
+      } else {  // through shared memory (A is not needed any more)
+        float* tile = reinterpret_cast<float*>(gram_at + warp * 4096);
+        const Block b{row - lane, s, c, l, z};
+        float4 w[8];
+        if (p.vec && p.weight) load_weights(p, b, lane, w);
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          *reinterpret_cast<float4*>(tile + lane * 32 + ((q ^ (lane & 7)) << 2)) =
+              make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        __syncwarp();
+        if (p.vec)
+          store_result4(p, b, lane, tile, w);
+        else
+          store_result1(p, b, lane, tile);
+      }
+    }
+  }
+
+  tc_fence_before();
+  cluster_sync();  // the pair's products and reads are done
+  tc_fence_after();
+  if (warp == kEpiWarps) tmem_dealloc_pair(tmem, TM);
+  cluster_sync();  // the collective release is complete in both CTAs
+}
+
 // ------------------------------------------------------------- host side
 
 struct MuonWs {
@@ -959,6 +1232,27 @@ pace_status ns_max_clusters(int* out) {
   return PACE_OK;
 }
 
+pace_status launch_small(const UArgs& u, const NsArgs& n, int64_t batch, cudaStream_t st) {
+  constexpr int kMaxDevices = 64;
+  static bool done[kMaxDevices] = {};  // shared-memory opt-in made on that device
+  static std::mutex mu;
+  int dev = 0;
+  PACE_TRY_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return PACE_ERR_CUDA;
+  {
+    std::lock_guard<std::mutex> g(mu);
+    if (!done[dev]) {
+      PACE_TRY_CUDA(cudaFuncSetAttribute(newton_schulz_small_kernel,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         static_cast<int>(kSmallSmem)));
+      done[dev] = true;
+    }
+  }
+  newton_schulz_small_kernel<<<static_cast<unsigned>(2 * batch), kSmallThreads, kSmallSmem, st>>>(
+      u, n);
+  return last_launch_status();
+}
+
 pace_status check_params(const PaceMuonParams* q) {
   if (!q || q->steps < 1 || q->steps > 32) return PACE_ERR_INVALID_ARG;
   for (float v : {q->lr, q->momentum, q->weight_decay, q->scale, q->eps, q->coef[0], q->coef[1],
@@ -1004,6 +1298,7 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
   n.cc = q->coef[2];
   n.ctr = w.ctr;
 
+  if (n.l <= kSmallSide) return launch_small(u, n, batch, st);
   Maps m;
   const int64_t xbs = u.rows * w.ldx, cbs = n.s * w.lda;
   for (int i = 0; i < 2; ++i) {
