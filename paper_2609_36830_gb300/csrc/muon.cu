@@ -874,7 +874,9 @@ __global__ void __launch_bounds__(kElemThreads, 4) direction_kernel(const UArgs 
 //            MN-major, the B operand of C X.
 // C takes the place of the rows of X once X X^T is done; a step's result goes to the CTA's
 // own rows and to the columns of either CTA.
-constexpr int kSmallThreads = 32 * (kEpiWarps + 1);
+constexpr int kSmallWarps = 16;  // four for each quarter of the rows, 64 columns each
+constexpr int kSmallThreads = 32 * kSmallWarps;
+constexpr int kSmallCols = 64;
 constexpr uint32_t kRegion = 65536;
 constexpr size_t kSmallSmem = 1024 + 3 * kRegion + 256;
 constexpr int kSmallSide = 256;
@@ -891,7 +893,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* pair_sum = reinterpret_cast<float*>(tmem_slot + 2);   // [2] the CTAs' squares
-  float* warp_sum = pair_sum + 2;                              // [kEpiWarps]
+  float* warp_sum = pair_sum + 2;                              // [kSmallWarps]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t crank = cluster_ctarank();
@@ -905,7 +907,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
     fence_barrier_init();
   }
   cluster_sync();  // both CTAs run and their barriers exist
-  if (warp == kEpiWarps) {
+  if (warp == 0) {
     tmem_alloc_pair(tmem_slot, TM);
     tmem_relinquish_pair();
   }
@@ -914,36 +916,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  // Thread of the epilogue: row of X, and 128 of its columns.
-  const int quad = warp & 3, side = warp >> 2;
+  // Thread of the epilogue: row of X, and 64 of its columns, which CTA `owner` has as columns.
+  const int quad = warp & 3, c_begin = (warp >> 2) * kSmallCols;
+  const uint32_t owner = static_cast<uint32_t>(c_begin / BM);
   const int row_l = quad * 32 + lane;
   const int row = static_cast<int>(crank) * BM + row_l;
-  // U's values at 32 columns of the thread's row (zeros outside), momentum updated if kNorm
-  auto load_u = [&](int col0, bool update, float (&v)[32]) {
+  // U's values at 32 columns of the thread's row (zeros outside); the momentum is updated
+  auto load_u = [&](int col0, float (&v)[32]) {
     if (!p.tall && u.vec && row < s) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (col0 + 8 * q < l) {
-          if (update) direction8<true>(u, z, row, col0 + 8 * q, f);
-          else direction8<false>(u, z, row, col0 + 8 * q, f);
-        }
+        if (col0 + 8 * q < l) direction8<true>(u, z, row, col0 + 8 * q, f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[8 * q + i] = f[i];
       }
       return;
     }
+    // X[row][col] is U[col][row] of a tall U: a warp's lanes read one of its rows
+    const int64_t ur = p.tall ? col0 : row, uc = p.tall ? row : col0;
+    const int64_t g_at = z * u.bs + ur * u.ld + uc, g_step = p.tall ? u.ld : 1;
+    const int64_t m_at = (z * u.rows + ur) * u.cols + uc, m_step = p.tall ? u.cols : 1;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const int col = col0 + i;
-      v[i] = 0.0f;
-      if (row >= s || col >= l) continue;
-      const int64_t ur = p.tall ? col : row, uc = p.tall ? row : col;
-      v[i] = load1(u, z * u.bs + ur * u.ld + uc);
-      if (u.momentum) {
-        float* mp = u.momentum + (z * u.rows + ur) * u.cols + uc;
-        float m = *mp;
-        if (update) *mp = m = fmaf(u.mu, m, v[i]);
+    for (int i = 0; i < 32; ++i)
+      v[i] = row < s && col0 + i < l ? load1(u, g_at + i * g_step) : 0.0f;
+    if (u.momentum) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        if (row >= s || col0 + i >= l) continue;
+        float* mp = u.momentum + m_at + i * m_step;
+        const float m = fmaf(u.mu, *mp, v[i]);
+        *mp = m;
         v[i] = direction(u, v[i], m);
       }
     }
@@ -958,56 +961,60 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
           make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
   };
   // the same 32 columns of X for the B operand of C X, in the CTA that holds the columns
-  const uint32_t cols_peer = cluster_addr(cols_at, static_cast<uint32_t>(side));
+  const bool own = owner == crank;
+  const uint32_t cols_peer = cluster_addr(cols_at, owner);
   auto put_columns = [&](int col0, const uint32_t (&h)[16]) {
-    const int n = col0 - side * BM;
-    const uint32_t at = cols_peer + (row >> 6) * 16384 + (n >> 6) * 8192 + (row & 63) * 128;
+    const int n = col0 & (BM - 1);
+    const uint32_t off = (row >> 6) * 16384 + (n >> 6) * 8192 + (row & 63) * 128;
     const int q0 = (n & 63) >> 3;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(
-                       at + (((q0 + q) ^ (row & 7)) << 4)),
-                   "r"(h[4 * q]), "r"(h[4 * q + 1]), "r"(h[4 * q + 2]), "r"(h[4 * q + 3])
-                   : "memory");
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t at = off + (((q0 + q) ^ (row & 7)) << 4);
+      const uint4 w = make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+      if (own)
+        *reinterpret_cast<uint4*>(cols_at + at) = w;
+      else
+        asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(cols_peer + at),
+                     "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w)
+                     : "memory");
+    }
   };
 
   // The norm: squares of the thread, the warp, the CTA, the pair.
-  if (warp < kEpiWarps) {
-    float ss = 0.0f;
-#pragma unroll 1
-    for (int c = side * BM; c < side * BM + BM && c < l; c += 32) {
-      float v[32];
-      load_u(c, true, v);
-      float part = 0.0f;
+  float first[2][32];  // the thread's columns of U
+  float ss = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) part = fmaf(v[i], v[i], part);
-      ss += part;
-    }
+  for (int k = 0; k < 2; ++k) load_u(c_begin + 32 * k, first[k]);
 #pragma unroll
-    for (int x = 16; x > 0; x >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, x);
-    if (lane == 0) warp_sum[warp] = ss;
+  for (int k = 0; k < 2; ++k) {
+    float part = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) part = fmaf(first[k][i], first[k][i], part);
+    ss += part;
   }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, x);
+  if (lane == 0) warp_sum[warp] = ss;
   __syncthreads();
   if (threadIdx.x < 2) {
     float sum = 0.0f;
-    for (int w = 0; w < kEpiWarps; ++w) sum += warp_sum[w];
+    for (int w = 0; w < kSmallWarps; ++w) sum += warp_sum[w];
     st_cluster_u32(cluster_addr(&pair_sum[crank], threadIdx.x), __float_as_uint(sum));
   }
   cluster_sync();
   const float norm = sqrtf(pair_sum[0] + pair_sum[1]);
   const float scale = p.sx / (norm + u.eps);
   if (!(norm < INFINITY) && crank == 0 && threadIdx.x == 0) report(p.status, PACE_ERR_NAN_INPUT);
-  if (warp < kEpiWarps) {
-#pragma unroll 1
-    for (int c = side * BM; c < side * BM + BM && c < kl * BK; c += 32) {
-      float v[32];
-      load_u(c, false, v);
-      uint32_t h[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i] * scale, v[2 * i + 1] * scale);
-      put_rows(rows_at, c, h);
-      put_columns(c, h);
-    }
+  for (int k = 0; k < 2; ++k) {
+    const int c = c_begin + 32 * k;
+    if (c >= kl * BK) break;
+    uint32_t h[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      h[i] = half2_rn(first[k][2 * i] * scale, first[k][2 * i + 1] * scale);
+    put_rows(rows_at, c, h);
+    put_columns(c, h);
   }
 
   bool ok = true;
@@ -1020,7 +1027,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
     tc_fence_before();
     cluster_sync();
     tc_fence_after();
-    if (warp == kEpiWarps) {
+    if (warp == 0) {  // one lane of the even CTA issues the product
       if (crank == 0 && elect_one()) {
         const uint32_t a_at = smem_u32(kind == kPoly ? gram_at : rows_at);
         const uint32_t b_at = smem_u32(kind == kStep ? cols_at : kind == kPoly ? gram_at : rows_at);
@@ -1038,7 +1045,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
         tc_commit_both(done);
       }
       __syncwarp();
-      continue;
     }
     if (ok && !__all_sync(0xffffffffu, mbar_wait_bounded(done, ph & 1, abort_flag))) {
       if (!*abort_flag) report(p.status, PACE_ERR_TIMEOUT);
@@ -1059,8 +1065,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
       f_acc = last ? 1.0f / (p.sc * p.sx) : 1.0f / p.sc;
     }
     const int width = last ? l : (kind == kStep ? kl : ks) * BK;
+    // (not unrolled: a quarter of the kernel's stalls are instructions on their way)
 #pragma unroll 1
-    for (int c = side * BM; c < side * BM + BM && c < width; c += 32) {
+    for (int c = c_begin; c < c_begin + kSmallCols && c < width; c += 32) {
       float v[32];
       tmem_ld_32x32b_x32(tbase + c, v);
       tmem_wait_ld();
@@ -1128,7 +1135,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
   tc_fence_before();
   cluster_sync();  // the pair's products and reads are done
   tc_fence_after();
-  if (warp == kEpiWarps) tmem_dealloc_pair(tmem, TM);
+  if (warp == 0) tmem_dealloc_pair(tmem, TM);
   cluster_sync();  // the collective release is complete in both CTAs
 }
 
