@@ -679,9 +679,9 @@ PACE_API void pace_muon_params_default(PaceMuonParams* p);
  * lr, momentum, weight_decay, scale and nesterov are not used.  A zero matrix stays
  * zero.  A norm that is infinite or NaN reports PACE_ERR_NAN_INPUT (squares are
  * float32: entries of 1e19 overflow).  Coefficients under which the steps diverge
- * give PACE_ERR_INVALID_ARG.  Three launches, one of them cooperative: it needs the
- * GPU's SMs to itself once they are free, and its waits are bounded (2 s, then
- * PACE_ERR_TIMEOUT). */
+ * give PACE_ERR_INVALID_ARG.  Matrices up to 256 x 256 take one launch; others three, one
+ * of them cooperative: it needs the GPU's SMs to itself once they are free, and its waits
+ * are bounded (2 s, then PACE_ERR_TIMEOUT). */
 PACE_API pace_status pace_orthogonalize(const void* x, int32_t dtype, int64_t batch,
                                         int64_t rows, int64_t cols, int64_t row_stride,
                                         int64_t batch_stride, const PaceMuonParams* params,
@@ -704,7 +704,9 @@ PACE_API pace_status pace_muon_update(float* weight, void* weight_bf16, const vo
                                       void* workspace, size_t workspace_bytes,
                                       int32_t* status_dev, void* stream);
 
-/* Workspace of both: two copies of X and one of A and B in fp16, and partial sums. */
+/* Workspace of both: two copies of X and one of the s x s products in fp16, partial sums
+ * and, where one side is many times the other, up to 20 MB of partial products (so a
+ * long matrix may need more than a larger square one). */
 PACE_API size_t pace_muon_workspace_size(int64_t batch, int64_t rows, int64_t cols);
 
 /* ------------------------------------------------------------------------ */

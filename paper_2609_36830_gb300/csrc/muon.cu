@@ -58,8 +58,8 @@ constexpr uint32_t kOutBytes = kEpiWarps * 2 * kOutTile;
 constexpr size_t kSmemBytes = 1024 + STAGES * kStageBytes + kOutBytes + 256;
 constexpr int kMaxClusters = 76;
 
-// A phase's product.
-enum { kGram = 0, kPoly = 1, kStep = 2 };
+// A phase's product; kReduce adds up the parts of a split X X^T.
+enum { kGram = 0, kPoly = 1, kStep = 2, kReduce = 3 };
 
 struct Maps {
   CUtensorMap x128[2], x64[2], a128, a64, c128, c64;  // loads: boxes of 64 x 128 and 64 x 64
@@ -73,6 +73,8 @@ struct NsArgs {
   int64_t ldx, lda;        // row pitch of X, and of A and C
   int64_t x_rows;          // rows of X
   __half* a;
+  int split;               // parts that X X^T's tiles are split into along l
+  float* part;             // [tile][part][64 blocks][32 columns][32 rows], or null
   float ca, cb, cc;        // the coefficients
   float sx, sa, sc;        // powers of two: X, A and C are held times these
   unsigned* ctr;           // arrivals at the grid barriers, zero at launch
@@ -131,6 +133,18 @@ __host__ __device__ inline Deal deal_tiles(int64_t tiles, int n_clusters) {
   return d;
 }
 
+// Parts along l for the tiles of X X^T.  Few tiles of a long X would leave most pairs idle
+// for l / 64 K steps of 0.25 us; in n parts they take an n-th of that and another phase, some
+// 5 us, which reads n parts one after the other, so n is at most the root of the K steps.
+// (256 x 14,336: 365 us in one part, 177 in 14, 650 in 56; 100 x 5,000 188 in one and 144 in
+// 8.)  From kMaxClusters, so that the workspace does not depend on the device.
+__host__ __device__ inline int gram_split(int64_t tiles, int64_t l) {
+  const int64_t nkb = (l + BK - 1) / BK;
+  int64_t n = 1;
+  while ((n + 1) * (n + 1) <= nkb && (n + 1) * tiles <= kMaxClusters) ++n;
+  return n >= 2 && nkb - nkb * 4 / (3 * n) >= 32 ? static_cast<int>(n) : 1;
+}
+
 // Tiles of a symmetric product (on and below the diagonal), and of the step, in a matrix.
 __host__ __device__ inline int64_t sym_tiles(int64_t s) {
   const int64_t t = (s + TM - 1) / TM;
@@ -141,15 +155,17 @@ __host__ __device__ inline int64_t step_tiles(int64_t s, int64_t l) {
 }
 
 // A phase's item: its matrix, the tile's row and column (in 256s), its first column and
-// how many (256 or 128).
+// how many (256 or 128), its K steps.
 struct Item {
   int z, i, j;
   int32_t n0, tn;
+  int k0, k1;
 };
 constexpr int kBlocksPerTile = TM / BK;
 
 struct Phase {
   int kind, cur;           // cur: which X is read
+  int split;               // parts of its tiles
   bool sym, last;          // last: the epilogue holds the result
   int ti, tj, per;         // tiles of rows and columns, tiles of a matrix
   Deal deal;
@@ -161,8 +177,10 @@ struct Phase {
   bool a_sym, b_sym, a_mn, b_mn;
 
   __device__ Phase(const NsArgs& p, const Maps& m, int ph, int n_clusters) {
-    kind = ph % 3;
-    const int step = ph / 3;
+    const int per_step = p.split > 1 ? 4 : 3;
+    const int r = ph % per_step, step = ph / per_step;
+    kind = r == 0 ? kGram : per_step == 3 ? r : r == 1 ? kReduce : r - 1;
+    split = kind == kGram ? p.split : 1;
     last = kind == kStep && step == p.steps - 1;
     cur = step & 1;
     const int ts = static_cast<int>((p.s + TM - 1) / TM), tl = static_cast<int>((p.l + TM - 1) / TM);
@@ -171,10 +189,14 @@ struct Phase {
     tj = sym || p.tall ? ts : tl;
     per = sym ? ts * (ts + 1) / 2 : ti * tj;
     deal = deal_tiles(static_cast<int64_t>(per) * p.batch, n_clusters);
+    if (split > 1) {
+      deal.items = deal.full = static_cast<int64_t>(per) * p.batch * split;
+      deal.halves = 1;
+    }
     nkb = static_cast<int>(((kind == kGram ? p.l : p.s) + BK - 1) / BK);
     cols = sym || p.tall ? p.s : p.l;
     a_mn = b_mn = a_sym = b_sym = false;
-    if (kind == kGram) {
+    if (kind == kGram || kind == kReduce) {
       ma128 = mb128 = &m.x128[cur];
       ma64 = mb64 = &m.x64[cur];
       a_mn = b_mn = p.tall;
@@ -208,17 +230,13 @@ struct Phase {
 
   // CTAs that have items: only they write, and arrive at the barrier that ends the phase.
   __device__ unsigned arrivals(int n_clusters) const {
+    if (kind == kReduce) return 2u * n_clusters;
     return 2u * static_cast<unsigned>(deal.items < n_clusters ? deal.items : n_clusters);
   }
 
-  __device__ Item item(int64_t t) const {
+  // A tile as one item.
+  __device__ Item whole(int64_t tile) const {
     Item it;
-    int64_t tile = t;
-    int half = -1;
-    if (t >= deal.full && deal.halves == 2) {
-      tile = deal.full + (t - deal.full) / 2;
-      half = static_cast<int>((t - deal.full) & 1);
-    }
     it.z = static_cast<int>(tile / per);
     const int r = static_cast<int>(tile - static_cast<int64_t>(it.z) * per);
     if (sym) {  // row by row of the lower triangle
@@ -232,8 +250,26 @@ struct Phase {
       it.i = rows_fast ? r % ti : r / tj;
       it.j = rows_fast ? r / ti : r % tj;
     }
-    it.n0 = it.j * TM + (half > 0 ? TM / 2 : 0);
-    it.tn = half >= 0 ? TM / 2 : TM;
+    it.n0 = it.j * TM;
+    it.tn = TM;
+    it.k0 = 0;
+    it.k1 = nkb;
+    return it;
+  }
+
+  __device__ Item item(int64_t t) const {
+    if (split > 1) {
+      const int64_t tile = t / split;
+      const int part = static_cast<int>(t - tile * split);
+      Item it = whole(tile);
+      it.k0 = nkb * part / split;
+      it.k1 = nkb * (part + 1) / split;
+      return it;
+    }
+    if (t < deal.full || deal.halves == 1) return whole(t);
+    Item it = whole(deal.full + (t - deal.full) / 2);
+    it.n0 += (t - deal.full) & 1 ? TM / 2 : 0;
+    it.tn = TM / 2;
     return it;
   }
 };
@@ -337,7 +373,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const uint32_t crank = cluster_ctarank();
   const bool leader = crank == 0;
   const int cid = static_cast<int>(blockIdx.x) / 2, n_clusters = static_cast<int>(gridDim.x) / 2;
-  const int n_phases = 3 * p.steps;
+  const int n_phases = (p.split > 1 ? 4 : 3) * p.steps;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -377,7 +413,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int ph = 0; ph < n_phases && ok; ++ph) {
       const Phase f(p, maps, ph, n_clusters);
-      if (cid < f.deal.items) {
+      if (f.kind == kReduce || cid < f.deal.items) {
         // what this phase reads is written
         const bool go = lane != 0 || ph == 0 || wait_phase(p.ctr, before, abort_flag);
         if (!__all_sync(0xffffffffu, go)) {
@@ -388,13 +424,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive(opened);
       }
       before += f.arrivals(n_clusters);
+      if (f.kind == kReduce) continue;
       for (int64_t t = cid; t < f.deal.items && ok; t += n_clusters) {
         const Item im = f.item(t);
         if (im.n0 >= f.cols) continue;  // the second half of a narrow last tile
         const int32_t ra = im.i * TM + static_cast<int32_t>(crank) * BM;
         const int32_t rb = im.n0 + static_cast<int32_t>(crank) * (im.tn / 2);
         const uint32_t bytes = 2 * (kStageA + im.tn * BK);
-        for (int kb = 0; kb < f.nkb; ++kb, ++it) {
+        for (int kb = im.k0; kb < im.k1; ++kb, ++it) {
           const uint32_t s = it % STAGES, par = (it / STAGES) & 1u;
           // this lane's box: K-major 64 (K) x 128 or 64 rows; MN-major 64 x 64 (K), one or two
           const bool a_mn = f.a_mn_at(im, kb), b_mn = f.b_mn_at(im, kb);
@@ -441,6 +478,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       bool ok = true;
       for (int ph = 0; ph < n_phases && ok; ++ph) {
         const Phase f(p, maps, ph, n_clusters);
+        if (f.kind == kReduce) continue;
         for (int64_t t = cid; t < f.deal.items && ok; t += n_clusters) {
           const Item im = f.item(t);
           if (im.n0 >= f.cols) continue;
@@ -453,7 +491,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           }
           tc_fence_after();
           const uint32_t d_tmem = tmem_base + acc * TM;
-          for (int kb = 0; kb < f.nkb; ++kb, ++it) {
+          for (int kb = im.k0; kb < im.k1; ++kb, ++it) {
             const uint32_t s = it % STAGES, par = (it / STAGES) & 1u;
             if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], par, abort_flag))) {
               ok = false;
@@ -470,7 +508,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int k = 0; k < BK / 16; ++k)
                 tc_mma_f16_pair(d_tmem, a + k * da, b + k * db, idesc,
-                                (kb > 0 || k > 0) ? 1u : 0u);
+                                (kb > im.k0 || k > 0) ? 1u : 0u);
               tc_commit_both(&empty[s]);
             }
             __syncwarp();
@@ -499,8 +537,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int ph = 0; ph < n_phases && ok; ++ph) {
       const Phase f(p, maps, ph, n_clusters);
-      if (cid >= f.deal.items) continue;
-      // A is read below
+      if (f.kind != kReduce && cid >= f.deal.items) continue;
+      // A or the parts are read below
       if (!__all_sync(0xffffffffu, mbar_wait_bounded(opened, n_open & 1u, abort_flag))) {
         give_up();
         ok = false;
@@ -512,7 +550,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           f.kind == kGram ? &maps.as : f.kind == kPoly ? &maps.cs : &maps.xs[f.cur ^ 1];
       // value = f_acc * accumulator (+ f_src * A + diag on the diagonal)
       float f_acc, f_src = 0.0f, diag = 0.0f;
-      if (f.kind == kGram) {
+      if (f.kind == kGram || f.kind == kReduce) {
         f_acc = p.sa / (p.sx * p.sx);
       } else if (f.kind == kPoly) {
         f_acc = p.cc * p.sc / (p.sa * p.sa);
@@ -521,7 +559,63 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       } else {
         f_acc = f.last ? 1.0f / (p.sc * p.sx) : 1.0f / p.sc;
       }
-      for (int64_t t = cid; t < f.deal.items; t += n_clusters) {
+      // 32 rows x 64 columns leave as one TMA tile of 128-byte rows (128-byte swizzle: the
+      // lanes' 16-byte stores are conflict-free), two in turn
+      auto tile_begin = [&]() {
+        if (lane == 0) bulk_wait_read<1>();
+        __syncwarp();
+        return stage + (n_out++ & 1u) * kOutTile;
+      };
+      auto tile_put = [&](unsigned char* tile, int k, const float (&v)[32]) {
+        uint32_t h[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<uint4*>(tile + lane * 128 + (((4 * k + q) ^ (lane & 7)) << 4)) =
+              make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+      };
+      auto tile_end = [&](unsigned char* tile, const CUtensorMap* to, int64_t col, int64_t row,
+                          int z) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_3d(to, tile, static_cast<int32_t>(col), static_cast<int32_t>(row), z);
+          bulk_commit();
+        }
+      };
+      if (f.kind == kReduce) {  // a warp per 32 rows x 16 columns, the parts in order
+        const int64_t n_units = static_cast<int64_t>(f.per) * p.batch * 128;
+        for (int64_t w = static_cast<int64_t>(blockIdx.x) * kEpiWarps + warp - 2; w < n_units;
+             w += static_cast<int64_t>(gridDim.x) * kEpiWarps) {
+          const int64_t tile_no = w / 128;
+          const int unit = static_cast<int>(w % 128);  // 8 blocks of rows, 16 of columns
+          const Item im = f.whole(tile_no);
+          const int64_t row0 = static_cast<int64_t>(im.i) * TM + unit / 16 * 32;
+          const int64_t col0 = im.n0 + unit % 16 * 16;
+          if (row0 >= rows || col0 >= f.cols) continue;
+          float v[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+          const float* at = p.part + (tile_no * p.split * 64 + unit / 2) * 1024 +
+                            (unit & 1) * 512 + lane;
+#pragma unroll 4
+          for (int s = 0; s < p.split; ++s, at += 64 * 1024)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] += __ldcg(at + 32 * i);
+          if (row0 + lane < rows) {
+            uint32_t h[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = half2_rn(v[2 * i] * f_acc, v[2 * i + 1] * f_acc);
+            uint4* to = reinterpret_cast<uint4*>(
+                p.a + (static_cast<int64_t>(im.z) * p.s + row0 + lane) * p.lda + col0);
+            to[0] = make_uint4(h[0], h[1], h[2], h[3]);
+            to[1] = make_uint4(h[4], h[5], h[6], h[7]);
+          }
+        }
+        fence_proxy_async();  // the next phase's TMA reads these stores
+      }
+      for (int64_t t = cid; f.kind != kReduce && t < f.deal.items; t += n_clusters) {
         const Item im = f.item(t);
         if (im.n0 >= f.cols) continue;
         const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
@@ -563,16 +657,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         };
         if (mine == 0) {
           release();
+        } else if (f.split > 1) {  // a part of a tile, as it is
+          float* at = p.part + (t * 64 + (crank * 4 + quad) * 8 + c_begin / 32) * 1024 + lane;
+#pragma unroll 1
+          for (int c = 0; c < mine; c += 32, at += 1024) {
+            float v[32];
+            tmem_ld_32x32b_x32(tbase + c_begin + c, v);
+            tmem_wait_ld();
+            if (c + 32 >= mine) release();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) __stcg(at + 32 * i, v[i]);
+          }
         } else if (!f.last) {
 #pragma unroll 1
           for (int c0 = c_begin; c0 < c_begin + mine; c0 += 64) {
             const int64_t col0 = im.n0 + c0;
             if (f.kind == kPoly && c0 != c_begin) load_a(c0);
-            // 32 rows x 64 columns leave as one TMA tile of 128-byte rows (128-byte
-            // swizzle: the lanes' 16-byte stores are conflict-free), two in turn
-            if (lane == 0) bulk_wait_read<1>();
-            __syncwarp();
-            unsigned char* tile = stage + (n_out++ & 1u) * kOutTile;
+            unsigned char* tile = tile_begin();
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               float v[32];
@@ -599,21 +700,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     if (lane == i) v[i] += diag;
                 }
               }
-              uint32_t h[16];
-#pragma unroll
-              for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i], v[2 * i + 1]);
-#pragma unroll
-              for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<uint4*>(tile + lane * 128 + (((4 * k + q) ^ (lane & 7)) << 4)) =
-                    make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+              tile_put(tile, k, v);
             }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              tma_store_3d(store, tile, static_cast<int32_t>(col0), static_cast<int32_t>(row_w),
-                           im.z);
-              bulk_commit();
-            }
+            tile_end(tile, store, col0, row_w, im.z);
           }
         } else {
           // The update.  Through shared memory, so that the warp's accesses to the
@@ -1144,6 +1233,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
 struct MuonWs {
   __half *x[2], *a, *c;
   float* partial;
+  float* part;   // X X^T in parts
+  int split;
   unsigned* ctr;
   int64_t ldx, lda;
 };
@@ -1159,6 +1250,9 @@ void carve_muon_ws(Carver& cv, int64_t batch, int64_t rows, int64_t cols, MuonWs
   w->c = cv.take<__half>(na);
   w->partial = cv.take<float>(static_cast<size_t>(batch) * elem_blocks(batch > 0 ? batch : 1, rows, cols));
   w->ctr = cv.take<unsigned>(1);
+  const int64_t tiles = batch * sym_tiles(s);
+  w->split = tiles > 0 ? gram_split(tiles, rows < cols ? cols : rows) : 1;
+  w->part = w->split > 1 ? cv.take<float>(static_cast<size_t>(tiles) * w->split * TM * TM) : nullptr;
 }
 
 // The largest |a x + b x^3 + c x^5| over 0 <= x <= r.
@@ -1304,6 +1398,8 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
   n.cb = q->coef[1];
   n.cc = q->coef[2];
   n.ctr = w.ctr;
+  n.split = w.split;
+  n.part = w.part;
 
   if (n.l <= kSmallSide) return launch_small(u, n, batch, st);
   Maps m;
@@ -1335,8 +1431,9 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
   PACE_TRY(last_launch_status());
 
   // as many pairs as the phase of most items can use (its tiles as halves)
-  const int64_t tiles = step_tiles(n.s, n.l) > sym_tiles(n.s) ? step_tiles(n.s, n.l) : sym_tiles(n.s);
-  const int64_t clusters = 2 * batch * tiles < max_clusters ? 2 * batch * tiles : max_clusters;
+  int64_t pairs = 2 * batch * step_tiles(n.s, n.l);
+  if (batch * sym_tiles(n.s) * n.split > pairs) pairs = batch * sym_tiles(n.s) * n.split;
+  const int64_t clusters = pairs < max_clusters ? pairs : max_clusters;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(2 * clusters), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);

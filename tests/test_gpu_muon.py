@@ -57,7 +57,8 @@ def check(got, want, rel=REL):
 @pytest.mark.parametrize("b,m,n", [
     (1, 8, 8), (1, 3, 300), (1, 300, 3), (2, 64, 64), (1, 65, 63), (3, 129, 130), (1, 255, 257),
     (1, 256, 256), (2, 300, 1000), (2, 1000, 300), (1, 513, 512), (1, 700, 3001), (1, 2731, 1023),
-    (5, 400, 400), (1, 2048, 2048)])
+    (5, 400, 400), (1, 2048, 2048), (1, 100, 5000), (1, 5000, 100), (2, 300, 6001), (1, 260, 14336),
+    (1, 3000, 257)])
 def test_orthogonalize(b, m, n, dtype):
     u = gauss(b, m, n, strong=max(1, min(m, n) // 16), dtype=dtype)
     status = pace.new_status(DEV)
