@@ -349,14 +349,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && leader) {
+    // The whole warp runs the loop and one lane issues: counters and descriptors are then
+    // the warp's, and a K step takes less of the issue that short products wait for.
+    if (leader) {
+      const bool issue = elect_one();
       uint32_t it = 0, tc = 0;
       bool ok = true;
       for (int64_t t = cid; t < n_items && ok; t += n_clusters, ++tc) {
         int kb0, kb1, part;
         work_of(t, &kb0, &kb1, &part);
         const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
-        if (!mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u, abort_flag)) {
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u,
+                                                               abort_flag))) {
           ok = false;
           break;
         }
@@ -364,30 +368,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
         const uint32_t d_tmem = tmem_base + acc * GBN;
         for (int kb = kb0; kb < kb1; ++kb, ++it) {
           const uint32_t s = it % GSTAGES, ph = (it / GSTAGES) & 1u;
-          if (!mbar_wait_bounded(&full[s], ph, abort_flag)) {
+          if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], ph, abort_flag))) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t sa = smem_u32(smem + s * kGStageBytes);
-          const uint32_t sb = sa + kGStageA;
+          const uint32_t sa = smem_u32(smem) + s * kGStageBytes;
+          const uint64_t a = operand_desc(sa, A_MN), b = operand_desc(sa + kGStageA, B_MN);
+          if (issue) {
 #pragma unroll
-          for (int k = 0; k < GBK / 16; ++k) {
-            const uint32_t ka = A_MN ? sa + k * 2048 : sa + k * 32;
-            const uint32_t kbb = B_MN ? sb + k * 2048 : sb + k * 32;
-            tc_mma_f16_pair(d_tmem, operand_desc(ka, A_MN), operand_desc(kbb, B_MN), kIdesc,
-                            (kb > kb0 || k > 0) ? 1u : 0u);
+            for (int k = 0; k < GBK / 16; ++k)  // (descriptors count in 16 bytes)
+              tc_mma_f16_pair(d_tmem, a + k * (A_MN ? 128 : 2), b + k * (B_MN ? 128 : 2), kIdesc,
+                              (kb > kb0 || k > 0) ? 1u : 0u);
+            tc_commit_both(&empty[s]);
           }
-          tc_commit_pair(cluster_addr(&empty[s], 0));
-          tc_commit_pair(cluster_addr(&empty[s], 1));
+          __syncwarp();
         }
         if (!ok) break;
-        tc_commit_pair(cluster_addr(&tmem_full[acc], 0));
-        tc_commit_pair(cluster_addr(&tmem_full[acc], 1));
+        if (issue) tc_commit_both(&tmem_full[acc]);
+        __syncwarp();
       }
-      if (!ok) give_up();
-      tc_commit_pair(cluster_addr(mma_done, 0));
-      mbar_wait_bounded(mma_done, 0, nullptr);
+      if (!ok && lane == 0) give_up();
+      __syncwarp();
+      if (issue) {
+        tc_commit_pair(cluster_addr(mma_done, 0));
+        mbar_wait_bounded(mma_done, 0, nullptr);
+      }
+      __syncwarp();
     }
   } else {
     const int quad = warp & 3;

@@ -199,13 +199,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && leader) {
+    // the whole warp runs the loop, one lane issues
+    if (leader) {
+      const bool issue = elect_one();
       constexpr uint32_t kIdesc = idesc_bf16_f32(2 * BM, N);
       uint32_t it = 0, tc = 0;
       bool ok = true;
       for (int t = cid; t < p.n_tiles && ok; t += n_clusters, ++tc) {
         const uint32_t acc = tc & 1u, acc_ph = (tc >> 1) & 1u;
-        if (!mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u, abort_flag)) {
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u,
+                                                               abort_flag))) {
           ok = false;
           break;
         }
@@ -213,27 +216,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const uint32_t d_tmem = tmem_base + acc * S::kAcc;
         for (int kb = 0; kb < nkb; ++kb, ++it) {
           const uint32_t s = it % S::kStages, ph = (it / S::kStages) & 1u;
-          if (!mbar_wait_bounded(&full[s], ph, abort_flag)) {
+          if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], ph, abort_flag))) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t sw = smem_u32(smem + s * S::kStage);
+          const uint32_t sw = smem_u32(smem) + s * S::kStage;
+          const uint64_t a = smem_desc_k128(sw), b = smem_desc_k128(sw + kStageW);
+          if (issue) {
 #pragma unroll
-          for (int k = 0; k < BK / 16; ++k)
-            tc_mma_f16_pair(d_tmem, smem_desc_k128(sw + k * 32),
-                            smem_desc_k128(sw + kStageW + k * 32), kIdesc,
-                            (kb > 0 || k > 0) ? 1u : 0u);
-          tc_commit_pair(cluster_addr(&empty[s], 0));
-          tc_commit_pair(cluster_addr(&empty[s], 1));
+            for (int k = 0; k < BK / 16; ++k)  // (descriptors count in 16 bytes)
+              tc_mma_f16_pair(d_tmem, a + 2 * k, b + 2 * k, kIdesc, (kb > 0 || k > 0) ? 1u : 0u);
+            tc_commit_both(&empty[s]);
+          }
+          __syncwarp();
         }
         if (!ok) break;
-        tc_commit_pair(cluster_addr(&tmem_full[acc], 0));
-        tc_commit_pair(cluster_addr(&tmem_full[acc], 1));
+        if (issue) tc_commit_both(&tmem_full[acc]);
+        __syncwarp();
       }
-      if (!ok) give_up();
-      tc_commit_pair(cluster_addr(mma_done, 0));
-      mbar_wait_bounded(mma_done, 0, nullptr);
+      if (!ok && lane == 0) give_up();
+      __syncwarp();
+      if (issue) {
+        tc_commit_pair(cluster_addr(mma_done, 0));
+        mbar_wait_bounded(mma_done, 0, nullptr);
+      }
+      __syncwarp();
     }
   } else {
     const int quad = warp & 3;

@@ -578,8 +578,10 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && leader) {
+    if (leader) {
       // ------------------------------------------------ MMA issuer (even CTA)
+      // (the whole warp runs the loop, one lane issues)
+      const bool issue = elect_one();
       uint32_t it = 0, tcount = 0;
       bool ok = true;
       while (ok && seg.load()) {
@@ -588,7 +590,8 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
           const uint32_t acc = tcount & 1u;
           const uint32_t acc_ph = (tcount >> 1) & 1u;
           ++tcount;
-          if (!mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u, abort_flag)) {
+          if (!__all_sync(0xffffffffu, mbar_wait_bounded_cluster(&tmem_empty[acc], acc_ph ^ 1u,
+                                                                 abort_flag))) {
             ok = false;
             break;
           }
@@ -597,31 +600,36 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
           for (int kb = 0; kb < nkb; ++kb, ++it) {
             const uint32_t s = it % STAGES;
             const uint32_t ph = (it / STAGES) & 1u;
-            if (!mbar_wait_bounded(&full[s], ph, abort_flag)) {
+            if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], ph, abort_flag))) {
               ok = false;
               break;
             }
             tc_fence_after();
-            const uint32_t sa = smem_u32(smem + a_tile_off(s));
-            const uint32_t sb = smem_u32(smem + b_tile_off(s));
+            const uint64_t da = smem_desc_k128(smem_u32(smem) + a_tile_off(s));
+            const uint64_t db = smem_desc_k128(smem_u32(smem) + b_tile_off(s));
+            if (issue) {
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k) {
-              tc_mma_f16_pair(d_tmem, smem_desc_k128(sa + k * 32), smem_desc_k128(sb + k * 32),
-                              kIdesc, (kb > 0 || k > 0) ? 1u : 0u);
+              for (int k = 0; k < BK / 16; ++k)  // (descriptors count in 16 bytes)
+                tc_mma_f16_pair(d_tmem, da + 2 * k, db + 2 * k, kIdesc,
+                                (kb > 0 || k > 0) ? 1u : 0u);
+              // the stage is free in both CTAs once these MMAs have read it
+              tc_commit_both(&empty[s]);
             }
-            // the stage is free in both CTAs once these MMAs have read it
-            tc_commit_pair(cluster_addr(&empty[s], 0));
-            tc_commit_pair(cluster_addr(&empty[s], 1));
+            __syncwarp();
           }
           if (!ok) break;
-          tc_commit_pair(cluster_addr(&tmem_full[acc], 0));
-          tc_commit_pair(cluster_addr(&tmem_full[acc], 1));
+          if (issue) tc_commit_both(&tmem_full[acc]);
+          __syncwarp();
         }
       }
-      if (!ok) give_up();
-      // all MMAs issued by this thread complete before tensor memory is freed
-      tc_commit_pair(cluster_addr(mma_done, 0));
-      mbar_wait_bounded(mma_done, 0, nullptr);
+      if (!ok && lane == 0) give_up();
+      __syncwarp();
+      // all MMAs issued by this warp complete before tensor memory is freed
+      if (issue) {
+        tc_commit_pair(cluster_addr(mma_done, 0));
+        mbar_wait_bounded(mma_done, 0, nullptr);
+      }
+      __syncwarp();
     }
   } else {
     // ------------------------------------------------ epilogue (4 warps, both CTAs)
