@@ -472,6 +472,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
         float v[32];
         tmem_ld_32x32b_x32(tbase + c, v);
         tmem_wait_ld();
+        if (c + 32 == GBN) {
+          // This warp has read its columns: one arrival on the even CTA's barrier, before
+          // the last stores.  (One that releases at cluster scope after them waits for
+          // the copies in flight.)
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_pair(acc ? empty1 : empty0);
+        }
         const int64_t col0 = n0 + c;
         if (kIsG) {
           if (row_w < M && col0 < p.g_cols) {  // M is a multiple of 32: all its rows
@@ -597,10 +605,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
           }
         }
       }
-      // one arrival per warp on the even CTA's barrier, after every lane's loads
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
     }
     if (lane == 0) bulk_wait_all();  // the copies are done before the CTA's memory goes
     __syncwarp();
