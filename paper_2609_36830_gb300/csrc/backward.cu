@@ -104,7 +104,7 @@ struct GemmArgs {
   // EPI_ACC
   void* acc_out;                // fp32 (EPI_ACC16: bf16, stored) [M][ldo]
   int acc_first;                // 1: store (the first chunk), 0: add
-  unsigned* round_ctr;          // pacing counter, zeroed before the launch (or null)
+  unsigned* round_ctr;          // pacing counter, zeroed before the call's launches (or null)
   int32_t* status;
 };
 
@@ -644,6 +644,7 @@ __global__ void __launch_bounds__(256)
     const int64_t n0 = nt * GBN;
     for (int c = lane * 4; c < GBN && n0 + c < p.N; c += 128) {  // N is a multiple of 64
       float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
       for (int s = 0; s < ts.splits; ++s) {
         const float4 x = __ldcg(reinterpret_cast<const float4*>(
             p.part + ((static_cast<int64_t>(s) * ts.tail + i) * (2 * GBM) + r) * GBN + c));
@@ -669,20 +670,6 @@ __global__ void to_bf16_kernel(const float4* __restrict__ in, uint4* __restrict_
     out[i] = make_uint4(bf16x2_rn(a.x, a.y), bf16x2_rn(a.z, a.w), bf16x2_rn(b.x, b.y),
                         bf16x2_rn(b.z, b.w));
   }
-}
-
-// Zero the gathered rows from n_valid up to the next multiple of GBM (at most
-// rows_end) of the compact buffer: dW reads whole GBM-row tiles of them, and the
-// rows outside the loss must contribute exactly 0 (0 x garbage could be NaN).
-__global__ void zero_tail_rows_kernel(uint4* __restrict__ buf, int64_t row_vecs,
-                                      const long long* __restrict__ n_valid, int64_t rows_end) {
-  const int64_t start = *n_valid;
-  int64_t end = (start + GBM - 1) / GBM * GBM;
-  if (end > rows_end) end = rows_end;
-  const int64_t total = (end - start) * row_vecs;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < total;
-       i += static_cast<int64_t>(gridDim.x) * blockDim.x)
-    buf[start * row_vecs + i] = make_uint4(0, 0, 0, 0);
 }
 
 // dLoss/dlp per row of the clipped surrogate (oracle: oracle_surrogate_grad), 0
@@ -942,7 +929,6 @@ pace_status launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUte
   // with partial tiles every cluster is launched: a short tail is spread over all
   const int64_t max_clusters = gemm_clusters();
   const int64_t grid = 2 * (items < max_clusters && !a.part ? items : max_clusters);
-  PACE_TRY_CUDA(cudaMemsetAsync(round_ctr, 0, sizeof(unsigned), st));
   a.round_ctr = round_ctr;
   gemm_kernel<A_MN, B_MN, EPI><<<static_cast<unsigned>(grid), kGemmThreads, kGSmemBytes, st>>>(
       ta, tb, tc, a);
@@ -958,7 +944,7 @@ pace_status launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUte
 struct BwWs {
   LmWs lm;            // compaction + gathered rows (hidden_c)
   uint16_t* g;        // bf16 G of one chunk, 64-column blocks [ceil(V / 64)][chunk][64]
-  unsigned* round_ctr;  // the GEMMs' pacing counter
+  unsigned* round_ctr;  // the GEMMs' pacing counters, three a chunk
   float* part;          // dH's partial tiles
   float* dw;            // bf16 gradients of several chunks: dW, added up in float32
 };
@@ -968,12 +954,16 @@ int64_t chunk_rows(int64_t n_rows) {
   return (c + GBM - 1) / GBM * GBM;
 }
 
+int64_t chunk_count(int64_t n_rows) {
+  return n_rows > kChunkRows ? (n_rows + kChunkRows - 1) / kChunkRows : 1;
+}
+
 void carve_bw_ws(Carver& cv, int64_t n_rows, int64_t n_seq, int H, int V, BwWs* w,
                  bool out16 = false) {
   carve_lm_ws(cv, n_rows, n_seq, H, true, &w->lm);
   const int64_t g_cols = (static_cast<int64_t>(V) + 63) / 64 * 64;
   w->g = cv.take<uint16_t>(static_cast<size_t>(chunk_rows(n_rows > 0 ? n_rows : 1)) * g_cols);
-  w->round_ctr = cv.take<unsigned>(1);
+  w->round_ctr = cv.take<unsigned>(static_cast<size_t>(3 * chunk_count(n_rows)));
   // a tail of R < kMaxGemmClusters tiles, and no more tiles than the rows have, in as many
   // parts as the vocabulary's K steps allow (none below 64 K steps: no tile is split then)
   const int64_t tiles = (chunk_rows(n_rows > 0 ? n_rows : 1) + 2 * GBM - 1) / (2 * GBM) *
@@ -1115,17 +1105,18 @@ pace_status backward_call(const PaceBatch* batch, const void* hidden, const void
   // the rows in the loss, gathered densely (always compacted here)
   PACE_TRY(run_compaction(batch, ws.lm.cw, AdvJob{}, nullptr, nullptr, nullptr, nullptr, nullptr,
                           status_dev, st));
-  PACE_TRY(run_gather(hidden, H, n_rows, ws.lm.cw, ws.lm.hidden_c, st));
   const int64_t rows_cap = n_rows > 128 ? n_rows : 128;
-  const int64_t row_vecs = static_cast<int64_t>(H) * 2 / 16;
-  zero_tail_rows_kernel<<<static_cast<unsigned>(sm_count() * 4), 256, 0, st>>>(
-      static_cast<uint4*>(ws.lm.hidden_c), row_vecs, ws.lm.cw.total, rows_cap);
-  PACE_TRY(last_launch_status());
+  // dW reads whole GBM-row tiles of them: the rows past their number must be exactly 0
+  // (0 x garbage could be NaN)
+  PACE_TRY(run_gather(hidden, H, n_rows, ws.lm.cw, ws.lm.hidden_c, st, GBM, rows_cap));
   const int64_t chunk = chunk_rows(n_rows);
   const int64_t g_cols = (static_cast<int64_t>(V) + 63) / 64 * 64;
   const int64_t g_blocks = g_cols / 64;
   // TMA row coordinates of the blocked G are 32-bit
   if (g_blocks * chunk > static_cast<int64_t>(INT32_MAX)) return PACE_ERR_UNSUPPORTED_SHAPE;
+  PACE_TRY_CUDA(cudaMemsetAsync(
+      ws.round_ctr, 0, static_cast<size_t>(3 * chunk_count(n_rows)) * sizeof(unsigned), st));
+  unsigned* round_ctr = ws.round_ctr;  // of the next GEMM
   for (int64_t c0 = 0; c0 < n_rows; c0 += chunk) {
     const int64_t rows_c = (n_rows - c0) < chunk ? (n_rows - c0) : chunk;
     const int64_t rows_c_pad = (rows_c + GBM - 1) / GBM * GBM;
@@ -1160,10 +1151,11 @@ pace_status backward_call(const PaceBatch* batch, const void* hidden, const void
       a.V = V;
       a.status = status_dev;
       if (dent)
-        PACE_TRY((launch_gemm<false, false, EPI_G_ENT>(ta, tb, tc, a, ws.round_ctr, st)));
+        PACE_TRY((launch_gemm<false, false, EPI_G_ENT>(ta, tb, tc, a, round_ctr, st)));
       else
-        PACE_TRY((launch_gemm<false, false, EPI_G>(ta, tb, tc, a, ws.round_ctr, st)));
+        PACE_TRY((launch_gemm<false, false, EPI_G>(ta, tb, tc, a, round_ctr, st)));
     }
+    ++round_ctr;
     // 2. dH rows = G W   (W read MN-major: [K = V][N = H])
     {
       CUtensorMap ta, tb;
@@ -1184,10 +1176,11 @@ pace_status backward_call(const PaceBatch* batch, const void* hidden, const void
       a.part = ws.part;
       a.status = status_dev;
       if (out16)
-        PACE_TRY((launch_gemm<false, true, EPI_ROWS16>(ta, tb, ta, a, ws.round_ctr, st)));
+        PACE_TRY((launch_gemm<false, true, EPI_ROWS16>(ta, tb, ta, a, round_ctr, st)));
       else
-        PACE_TRY((launch_gemm<false, true, EPI_ROWS>(ta, tb, ta, a, ws.round_ctr, st)));
+        PACE_TRY((launch_gemm<false, true, EPI_ROWS>(ta, tb, ta, a, round_ctr, st)));
     }
+    ++round_ctr;
     // 3. dW += G^T H_c, in float32 (a lone chunk's bf16 dW is stored as it is)   (G read MN-major: [K = rows][M = V]; H_c MN-major: [K = rows][N = H])
     {
       CUtensorMap ta, tb, tc;
@@ -1213,10 +1206,11 @@ pace_status backward_call(const PaceBatch* batch, const void* hidden, const void
       a.ldo = H;
       a.status = status_dev;
       if (dw16)
-        PACE_TRY((launch_gemm<true, true, EPI_ACC16>(ta, tb, tc, a, ws.round_ctr, st)));
+        PACE_TRY((launch_gemm<true, true, EPI_ACC16>(ta, tb, tc, a, round_ctr, st)));
       else
-        PACE_TRY((launch_gemm<true, true, EPI_ACC>(ta, tb, tc, a, ws.round_ctr, st)));
+        PACE_TRY((launch_gemm<true, true, EPI_ACC>(ta, tb, tc, a, round_ctr, st)));
     }
+    ++round_ctr;
   }
   if (ws.dw) {
     to_bf16_kernel<<<static_cast<unsigned>(sm_count() * 8), 256, 0, st>>>(

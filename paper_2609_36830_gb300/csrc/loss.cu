@@ -729,15 +729,23 @@ __global__ void __launch_bounds__(kFewThreads)
 }
 
 // Copy the hidden rows listed in rowidx into a dense buffer, one warp per row,
-// 16 bytes per lane per step.
+// 16 bytes per lane per step.  Rows from their number up to the next multiple of `pad`
+// (at most rows_end) are set to zero.
 __global__ void gather_rows_kernel(const uint4* __restrict__ hidden, int64_t row_vecs,
                                    const int32_t* __restrict__ rowidx,
-                                   const long long* __restrict__ n_in, uint4* __restrict__ out) {
+                                   const long long* __restrict__ n_in, int pad, int64_t rows_end,
+                                   uint4* __restrict__ out) {
   const long long m = *n_in;
+  int64_t end = (m + pad - 1) / pad * pad;
+  if (end > rows_end) end = rows_end;
   const int lane = threadIdx.x & 31;
   const int64_t warps = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 5;
-  for (int64_t r = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5; r < m;
-       r += warps) {
+  for (int64_t r = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> 5;
+       r < m || r < end; r += warps) {
+    if (r >= m) {
+      for (int64_t v = lane; v < row_vecs; v += 32) out[r * row_vecs + v] = make_uint4(0, 0, 0, 0);
+      continue;
+    }
     const uint4* src = hidden + static_cast<int64_t>(rowidx[r]) * row_vecs;
     uint4* dst = out + r * row_vecs;
     for (int64_t v = lane; v < row_vecs; v += 32) dst[v] = __ldg(src + v);
@@ -799,14 +807,14 @@ pace_status run_compaction(const PaceBatch* b, const CompactWs& ws, const AdvJob
 }
 
 pace_status run_gather(const void* hidden, int H, int64_t n_rows, const CompactWs& ws,
-                       void* out, cudaStream_t st) {
+                       void* out, cudaStream_t st, int pad, int64_t rows_end) {
   if (n_rows == 0) return PACE_OK;
   const int64_t row_vecs = static_cast<int64_t>(H) * 2 / 16;
   int64_t blocks = (n_rows + 7) / 8;
   const int64_t cap = static_cast<int64_t>(sm_count()) * 16;
   if (blocks > cap) blocks = cap;
   gather_rows_kernel<<<static_cast<unsigned>(blocks), 256, 0, st>>>(
-      static_cast<const uint4*>(hidden), row_vecs, ws.rowidx, ws.total,
+      static_cast<const uint4*>(hidden), row_vecs, ws.rowidx, ws.total, pad, rows_end,
       static_cast<uint4*>(out));
   return last_launch_status();
 }

@@ -96,7 +96,9 @@ RowCounts carve_row_counts(Carver& cv, int64_t n_rows);
 pace_status launch_count_rows(const PaceBatch* b, RowCounts counts, unsigned long long* seq_in,
                               int* n_used, const AdvJob& adv, unsigned* counter0,
                               unsigned* counter1, int32_t* status, cudaStream_t st);
+// The rows in the loss, densely; zeros from their number up to a multiple of `pad` rows, at
+// most rows_end.
 pace_status run_gather(const void* hidden, int H, int64_t n_rows, const CompactWs& ws,
-                       void* out, cudaStream_t st);
+                       void* out, cudaStream_t st, int pad = 1, int64_t rows_end = 0);
 
 }  // namespace pace
