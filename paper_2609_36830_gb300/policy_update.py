@@ -1,0 +1,92 @@
+"""One policy update after admission, from the rollout's logits to the new weights.
+
+A step of a policy whose last trainable matrix is a projection P [H, D] in front of a
+vocabulary head W [V, H] (hidden = x P^T, logits = hidden W^T):
+  record   the rollout engine's logits give the behaviour log-probs that the loss
+           needs, with entropies and alternatives for monitoring
+           (pace.logits_logprob);
+  forward  log-probs, entropies and the clipped surrogate of the rows in the loss
+           (pace.token_logprob_entropy; with head="logits" from logits in memory);
+  backward dLoss/dlp (pace.surrogate_backward), the entropy bonus, and their gradients
+           through the head (pace.token_logprob_entropy_backward, or
+           pace.logits_logprob_backward in the logits' own buffer);
+  update   P by momentum and Newton-Schulz orthogonalisation (pace.muon_update),
+           with the bf16 copy that the next forward reads.
+The projection itself, and the head's products with head="logits", stand for the caller's
+model: plain matrix products.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+from . import pace
+
+
+class PolicyUpdate:
+    """Weights, momentum and buffers of the update; ``step`` queues one update and
+    synchronises nothing.
+
+    entropy_coef adds -entropy_coef x (mean entropy of the rows in the loss) to the loss.
+    head: "fused" (logits never in memory) or "logits" (a head that needs them)."""
+
+    def __init__(self, proj, w_vocab, loss_params=None, muon=None, entropy_coef=0.0,
+                 temperature=1.0, group_size=8, head="fused"):
+        if head not in ("fused", "logits"):
+            raise ValueError(f"head: 'fused' or 'logits', not {head!r}")
+        # float32 weights [H, D], the object's own
+        self.proj = proj.detach().to(torch.float32, copy=True).contiguous()
+        self.proj16 = self.proj.to(torch.bfloat16)
+        self.momentum = torch.zeros_like(self.proj)
+        self.w = w_vocab
+        self.loss_params = loss_params or pace.loss_params()
+        h, d = self.proj.shape
+        self.muon = muon or pace.muon_params(scale=0.2 * math.sqrt(max(h, d)))
+        self.entropy_coef, self.temperature = float(entropy_coef), float(temperature)
+        self.group_size, self.head = int(group_size), head
+        self.ws_muon = pace.workspace(pace.muon_workspace_size(1, h, d), proj.device)
+        self.status = pace.new_status(proj.device)
+
+    def record(self, logits, targets, top_k=0, allowed=None):
+        """The rollout side: log-probs of the sampled tokens under the sampling
+        distribution (the loss's behav_lp), entropies and, with top_k, alternatives."""
+        return pace.logits_logprob(pace.make_logits(logits, allowed=allowed), targets,
+                                   self.temperature, top_k, status=self.status)
+
+    def step(self, x, seq_offsets, targets, behav_lp, reward, mask, seq_accepted=None):
+        """One update from features x [n_rows, D] (bf16).  mask: uint8 [n_rows], 1 where a
+        row is in the loss.  Returns dict loss (float64 [1]), logprob, entropy [n_rows],
+        grad_w (bf16 [V, H]) and grad_proj (float32 [H, D]) of the weights used."""
+        n_rows, dev, tau = x.shape[0], x.device, self.temperature
+        loss = torch.zeros(1, dtype=torch.float64, device=dev)
+        batch = pace.make_batch(seq_offsets, n_rows, seq_accepted=seq_accepted, mask=mask)
+        args = pace.make_loss_args(behav_lp, reward, self.group_size, self.loss_params, loss)
+        rows = mask.float()
+        if seq_accepted is not None:
+            rows = rows * torch.repeat_interleave(seq_accepted, torch.diff(seq_offsets),
+                                                  output_size=n_rows)
+        dentropy = rows * (-self.entropy_coef) / rows.sum().clamp(min=1.0)
+        hidden = x @ self.proj16.T
+        if self.head == "fused":
+            lp, lse, ent = pace.token_logprob_entropy(batch, hidden, self.w, targets, tau,
+                                                      loss=args, status=self.status)
+            dlp = pace.surrogate_backward(batch, lp, args, status=self.status)
+            grad_h, grad_w = pace.token_logprob_entropy_backward(
+                batch, hidden, self.w, targets, lse, dlp, entropy=ent, dentropy=dentropy,
+                temperature=tau, status=self.status)
+        else:
+            logits = hidden @ self.w.T
+            lg = pace.make_logits(logits, mask=rows.to(torch.uint8))
+            o = pace.logits_logprob(lg, targets, tau, status=self.status)
+            lp, ent = o["logprob"], o["entropy"]
+            pace.surrogate_loss(batch, lp, args, status=self.status)
+            dlp = pace.surrogate_backward(batch, lp, args, status=self.status)
+            g = pace.logits_logprob_backward(lg, targets, o["stats"], dlp, ent, dentropy, tau,
+                                             grad=logits, status=self.status)
+            grad_h, grad_w = g @ self.w, g.T @ hidden
+        grad_proj = (grad_h.T @ x).float()
+        pace.muon_update(self.proj, grad_proj, self.momentum, self.muon,
+                         weight_bf16=self.proj16, ws=self.ws_muon, status=self.status)
+        return {"loss": loss, "logprob": lp, "entropy": ent, "grad_w": grad_w,
+                "grad_proj": grad_proj}

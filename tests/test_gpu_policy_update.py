@@ -1,0 +1,114 @@
+"""The policy update end to end: gradients against 64-bit autograd of the same loss, both
+forms of the head, and a few steps that raise what is rewarded.
+
+bf16 hidden states, gradients G and dH are rounded to 2^-8 of themselves, twice on the way
+to the projection's gradient, and its products are bf16: 3 x 2^-8 of the norm."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_36830_gb300 import pace
+from paper_2609_36830_gb300.policy_update import PolicyUpdate
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def setup(n_seq=16, length=20, D=192, H=128, V=1003, seed=0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    n = n_seq * length
+    x = torch.randn(n, D, device=DEV, generator=g).to(torch.bfloat16)
+    p = torch.randn(H, D, device=DEV, generator=g) / math.sqrt(D)
+    w = (torch.randn(V, H, device=DEV, generator=g) * 2 / math.sqrt(H)).to(torch.bfloat16)
+    y = torch.randint(0, V, (n,), device=DEV, generator=g, dtype=torch.int32)
+    off = torch.arange(0, n + 1, length, device=DEV)
+    mask = (torch.rand(n, device=DEV, generator=g) < 0.7).to(torch.uint8)
+    acc = torch.ones(n_seq, dtype=torch.uint8, device=DEV)
+    acc[8:] = 0 if n_seq > 16 else 1
+    reward = torch.rand(n_seq, device=DEV, generator=g)
+    return x, p, w, y, off, mask, acc, reward
+
+
+@pytest.mark.parametrize("head", ["fused", "logits"])
+def test_gradients_and_recorded_log_probs(head):
+    x, p, w, y, off, mask, acc, reward = setup()
+    up = PolicyUpdate(p, w, entropy_coef=0.05, temperature=0.8, head=head)
+    hidden = x @ up.proj16.T
+    logits = hidden @ w.T
+    rec = up.record(logits, y, top_k=3)
+    behav = rec["logprob"] - 0.1 * torch.randn(len(y), device=DEV)
+    before = up.proj.clone()
+    o = up.step(x, off, y, behav, reward, mask, acc)
+    torch.cuda.synchronize()
+    assert int(up.status.item()) == 0
+    assert (up.proj != before).any() and torch.equal(up.proj16, up.proj.to(torch.bfloat16))
+
+    pd = before.to(torch.bfloat16).double().requires_grad_()
+    wd = w.double().requires_grad_()
+    # values as rounded on the way (hidden states, and logits that are in memory), derivatives
+    # as if they were not
+    hd = x.double() @ pd.T
+    hd = hd + (hidden.double() - hd).detach()
+    z = hd @ wd.T
+    if head == "logits":
+        z = z + (logits.double() - z).detach()
+    z = z / 0.8
+    lp_all = torch.log_softmax(z, 1)
+    lp = lp_all.gather(1, y.long()[:, None])[:, 0]
+    ent = -(lp_all.exp() * lp_all).sum(1)
+    m = mask.double()
+    adv = pace.group_advantages(reward, 8, seq_accepted=acc).double().repeat_interleave(20)
+    rho = torch.exp(lp - behav.double())
+    term = torch.maximum(-adv * rho, -adv * rho.clamp(0.8, 1.28))
+    loss = (m * term).sum() / m.sum()
+    (loss - 0.05 * (m * ent).sum() / m.sum()).backward()
+    inn = mask > 0
+    assert (o["logprob"] - lp).abs()[inn].max().item() < 0.05
+    assert (o["entropy"] - ent).abs()[inn].max().item() < 0.05
+    assert abs(o["loss"].item() - loss.item()) < 0.01
+    for got, want in ((o["grad_proj"], pd.grad), (o["grad_w"], wd.grad)):
+        rel = (got.double() - want).norm() / want.norm()
+        assert rel.item() < 3 * 2.0 ** -8 + 0.02, rel  # (and the clip's branches near its edge)
+
+
+def test_forms_of_the_head_agree():
+    x, p, w, y, off, mask, acc, reward = setup(seed=3)
+    outs = []
+    for head in ("fused", "logits"):
+        up = PolicyUpdate(p, w, entropy_coef=0.01, head=head)
+        behav = up.record((x @ up.proj16.T) @ w.T, y)["logprob"]
+        outs.append(up.step(x, off, y, behav, reward, mask, acc))
+    inn = mask > 0
+    # the logits in memory are bf16: 2^-9 of |z| < 10
+    assert (outs[0]["logprob"] - outs[1]["logprob"]).abs()[inn].max().item() < 0.05
+    rel = (outs[0]["grad_proj"] - outs[1]["grad_proj"]).norm() / outs[0]["grad_proj"].norm()
+    assert rel.item() < 0.05
+
+
+def test_rewarded_sequences_become_likelier():
+    """Ten updates on one batch: sequences above their group's mean gain log-prob on those
+    below, while the entropy bonus keeps the policy from collapsing."""
+    x, p, w, y, off, mask, acc, _ = setup(seed=5)
+    reward = torch.tensor([1.0, 0.0] * 8, device=DEV)
+    up = PolicyUpdate(p, w, muon=pace.muon_params(lr=0.01, scale=0.2 * math.sqrt(192)),
+                      entropy_coef=0.001)
+    behav = up.record((x @ up.proj16.T) @ w.T, y)["logprob"]
+    gap = []
+    for _ in range(10):
+        o = up.step(x, off, y, behav, reward, mask, acc)
+        lp = (o["logprob"] * mask).reshape(16, 20).sum(1)
+        gap.append((lp[0::2].mean() - lp[1::2].mean()).item())
+    assert int(up.status.item()) == 0
+    assert gap[-1] > gap[0] + 0.5, gap
+    assert torch.isfinite(up.proj).all() and o["entropy"][mask > 0].min().item() > 0.1
+
+
+def test_refusals():
+    x, p, w, y, off, mask, acc, reward = setup()
+    with pytest.raises(ValueError, match="head"):
+        PolicyUpdate(p, w, head="other")
+    up = PolicyUpdate(p, w)
+    with pytest.raises(ValueError, match="at least"):
+        up.step(x, off, y, torch.zeros(len(y), device=DEV), reward, mask[:-1])
