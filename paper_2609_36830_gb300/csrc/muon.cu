@@ -19,7 +19,7 @@
 // a grid barrier between them (a launch for each would add its start and drain to
 // products of 5-100 us).  In a phase the work items are 256 x 256 tiles, dealt to CTA
 // pairs (deal_tiles); per pair the structure of the other tensor-core kernels: warp 0 of
-// each CTA issues TMA loads of its 128 A rows and its half of the B tile into a 4-stage
+// each CTA issues TMA loads of its 128 A rows and its half of the B tile into a 5-stage
 // ring, warp 1 of the even CTA issues tcgen05.mma.cta_group::2 (M 256, N 256 or 128, K 16),
 // warps 2-9 of each CTA drain one of two accumulators while the next tile is computed.  A
 // and C are symmetric, so only tiles on and below the diagonal are computed and stored, and
@@ -46,7 +46,7 @@ namespace {
 constexpr int TM = 256;  // rows and columns of a pair's tile
 constexpr int BM = 128;  // rows of it per CTA
 constexpr int BK = 64;
-constexpr int STAGES = 4;
+constexpr int STAGES = 5;
 constexpr int kEpiWarps = 8;  // two for each quarter of the tensor memory's lanes
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr uint32_t kStageA = BM * BK * 2;      // 16 KB
@@ -57,6 +57,14 @@ constexpr uint32_t kOutTile = 32 * 128;        // an epilogue warp's staging til
 constexpr uint32_t kOutBytes = kEpiWarps * 2 * kOutTile;
 constexpr size_t kSmemBytes = 1024 + STAGES * kStageBytes + kOutBytes + 256;
 constexpr int kMaxClusters = 76;
+
+// A place in the ring: stage, and the parity of its use.
+struct Ring {
+  uint32_t s = 0, par = 0;
+  __device__ void next() {
+    if (++s == STAGES) s = 0, par ^= 1u;
+  }
+};
 
 // A phase's product; kReduce adds up the parts of a split X X^T.
 enum { kGram = 0, kPoly = 1, kStep = 2, kReduce = 3 };
@@ -408,7 +416,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == 0) {
     uint64_t pol;
     asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
-    uint32_t it = 0;
+    Ring ring;
+    uint32_t it = 0;  // stages filled
     unsigned before = 0;  // arrivals of the phases before this one
     bool ok = true;
     for (int ph = 0; ph < n_phases && ok; ++ph) {
@@ -431,8 +440,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int32_t ra = im.i * TM + static_cast<int32_t>(crank) * BM;
         const int32_t rb = im.n0 + static_cast<int32_t>(crank) * (im.tn / 2);
         const uint32_t bytes = 2 * (kStageA + im.tn * BK);
-        for (int kb = im.k0; kb < im.k1; ++kb, ++it) {
-          const uint32_t s = it % STAGES, par = (it / STAGES) & 1u;
+        for (int kb = im.k0; kb < im.k1; ++kb, ++it, ring.next()) {
+          const uint32_t s = ring.s, par = ring.par;
           // this lane's box: K-major 64 (K) x 128 or 64 rows; MN-major 64 x 64 (K), one or two
           const bool a_mn = f.a_mn_at(im, kb), b_mn = f.b_mn_at(im, kb);
           const int boxes_a = a_mn ? 2 : 1, boxes = boxes_a + (b_mn ? im.tn / 128 : 1);
@@ -474,7 +483,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     // (one lane running it alone took 0.31 us for a K step of four MMAs, whatever their N).
     if (leader) {
       const bool issue = elect_one();
-      uint32_t it = 0, tc = 0;
+      Ring ring;
+      uint32_t tc = 0;
       bool ok = true;
       for (int ph = 0; ph < n_phases && ok; ++ph) {
         const Phase f(p, maps, ph, n_clusters);
@@ -491,8 +501,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
           }
           tc_fence_after();
           const uint32_t d_tmem = tmem_base + acc * TM;
-          for (int kb = im.k0; kb < im.k1; ++kb, ++it) {
-            const uint32_t s = it % STAGES, par = (it / STAGES) & 1u;
+          for (int kb = im.k0; kb < im.k1; ++kb, ring.next()) {
+            const uint32_t s = ring.s, par = ring.par;
             if (!__all_sync(0xffffffffu, mbar_wait_bounded(&full[s], par, abort_flag))) {
               ok = false;
               break;
