@@ -611,8 +611,8 @@ typedef struct {
  *   top_ids, top_logprob [top_k]: the places of the largest logits, equal logits
  *             lowest place first, and their log-probs; -1 and -inf where the row
  *             has fewer places.
- * A row without places has logprob and lse -inf, entropy 0, stats {-inf, 0} and no
- * alternatives.  A row that holds NaN or +inf in a place that is not excluded has
+ * A row without places has logprob and lse -inf, entropy NaN (there is no distribution),
+ * stats {-inf, 0} and no alternatives; its gradient is 0.  A row that holds NaN or +inf in a place that is not excluded has
  * NaN in every float32 output (top_ids -1) and PACE_ERR_NAN_INPUT is reported; a
  * target outside the vocabulary has logprob NaN and PACE_ERR_INVALID_ARG.
  *   targets     device int32 [n_rows], or NULL together with logprob.

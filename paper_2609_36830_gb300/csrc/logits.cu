@@ -739,7 +739,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     }
     if (p.lse) p.lse[r] = bad ? nan : (empty ? -INFINITY : fmaf(all.m, p.inv_t, log_s));
     if (p.entropy)
-      p.entropy[r] = bad ? nan : (empty ? 0.0f : logf(all.s) - 0.69314718f * (all.t / all.s));
+      p.entropy[r] = bad || empty ? nan : logf(all.s) - 0.69314718f * (all.t / all.s);
     if (p.stats)
       reinterpret_cast<float2*>(p.stats)[r] =
           bad ? make_float2(nan, nan) : make_float2(all.m, log_s);

@@ -37,6 +37,7 @@ def reference(z, targets, t, k, allowed=None):
     lp = torch.where(empty, torch.full_like(d, -INF), d - torch.log(s))
     p = torch.exp(lp)
     ent = -torch.where(p > 0, p * lp, 0 * p).sum(1)
+    ent[empty[:, 0]] = math.nan  # no distribution
     lse = torch.where(empty[:, 0], torch.full_like(s[:, 0], -INF), (m / t)[:, 0] + torch.log(s)[:, 0])
     # by value, equal ones lowest place first: a stable sort of the negated values
     order = torch.sort(-(z + 0.0), dim=1, stable=True).indices[:, :k]
@@ -128,7 +129,7 @@ def test_allowed_places(dtype, V, keep):
     junk = torch.tensor([math.nan, INF, -INF])[torch.randint(0, 3, (R, V), generator=g)]
     z = torch.where(allowed, z, junk).to(dtype).to(DEV)
     o, _ = check_forward(z, 1.0, 20, allowed)
-    assert o["lse"][3].item() == -INF and o["entropy"][3].item() == 0.0
+    assert o["lse"][3].item() == -INF and math.isnan(o["entropy"][3].item())
     assert o["stats"][3, 0].item() == -INF and (o["top_ids"][3] == -1).all()
 
 
