@@ -520,8 +520,10 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
   const int c1 = static_cast<int>(static_cast<int64_t>(n_chunks) * (rank + 1) / C);
 
   // A warp takes kUnroll chunks at a time and has the next ones in flight.  Chunks all of
-  // whose vectors are whole, [f0, f1), are read without tests.
+  // whose vectors are whole, [f0, f1), are read without tests.  The maximum is the warp's,
+  // so that it grows in few of the turns and the lanes' sums are added up as they are.
   Sums a{-INFINITY, 0.0f, 0.0f};
+  float lane_max = -INFINITY;  // kTop: of the lane's logits
   const int f0 = row.shift ? 1 : 0, f1 = (row.shift + row.V) / kPer / 32;
   const uint4* const vectors = reinterpret_cast<const uint4*>(row.z - row.shift);
   uint4 next[kUnroll];
@@ -557,15 +559,16 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const float vm = Logit<T>::largest(raw[u]);
-        m = max_nan(m, vm);
+        lane_max = max_nan(lane_max, vm);
         const float cm = warp_max_nan(vm);
+        m = max_nan(m, cm);
         if (lane == 0 && c + u < c1) ckey[c + u - c0] = order_key(cm);
       }
     } else {
-      m = max_nan(m, Logit<T>::template largest_of<kUnroll>(raw));
+      m = max_nan(m, warp_max_nan(Logit<T>::template largest_of<kUnroll>(raw)));
     }
     const float ref = m == -INFINITY ? 0.0f : m;
-    if (ref != a.m) a = raised(a, ref, p.k);
+    if (m != a.m) a = raised(a, ref, p.k);  // (the same for the warp)
     a.m = m;
     const float c_ref = ref * p.k;
     if (ordinary(c_ref)) {
@@ -606,7 +609,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     return Sums{m, warp_sum(y2.s), warp_sum(y2.t)};
   };
   const Sums none{-INFINITY, 0.0f, 0.0f};
-  const Sums w = merge(a);
+  const Sums w{a.m, warp_sum(a.s), warp_sum(a.t)};
   if (lane == 0) s_warp[warp] = w;
   __syncthreads();
   if (warp == 0) {
@@ -631,7 +634,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     // The bound: the k-th largest of the maxima of `groups` groups of lanes.  With four
     // groups an alternative, about 1.15 k logits reach it in random order.
     const int lanes = bound_lanes(p.top, warps);
-    float lm = a.m;
+    float lm = lane_max;
     for (int x = 1; x < lanes; x <<= 1) lm = fmaxf(lm, __shfl_xor_sync(0xffffffffu, lm, x));
     const int groups = warps * 32 / lanes;
     if (lane % lanes == 0) s_top.group[(warp * 32 + lane) / lanes] = order_key(lm);
