@@ -830,23 +830,41 @@ __global__ void __launch_bounds__(kBwThreads) logits_backward_kernel(const Backw
       }
     }
   }
+  // -(g + e (ln p + H)) = x1 log2 p + x0
+  const float x0 = -fmaf(ge, h, gl), x1 = -0.69314718f * ge;
+  // log2 p is z k - (m k + log2 S), one fused multiply-add, where 16-bit gradients hide the
+  // constant's rounding; float32's would not, nor would a large m's.
+  const float c_all = fmaf(st.x, p.k, l2s);
+  const bool one_fma = kPer == 8 && ordinary(c_all);
 #pragma unroll
   for (int u = 0; u < kBwVecs; ++u) {
     const int v = v0 + u * kBwThreads;
     if (v >= n_vec) break;
     const int j0 = v * kPer - shift;
     float f[kPer];
-    Logit<T>::unpack(raw[u], f);
     if (live) {
+      if (kAllowed) raw[u] = Row<T>::masked(raw[u], bits[u]);
+      Logit<T>::unpack(raw[u], f);
+      // the target, unless it is excluded
+      const uint32_t at = static_cast<uint32_t>(y - j0);
+      bool hit = false;
+      if (at < static_cast<uint32_t>(kPer)) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (at == static_cast<uint32_t>(i)) hit = f[i] != -INFINITY;
+      }
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const float z = !kAllowed || (bits[u] >> i & 1u) ? f[i] : -INFINITY;
-        const float lp2 = fmaxf(fmaf(z - st.x, p.k, -l2s), -1e30f);  // log2 p, finite
+        // (finite, so that p x is 0 where p is)
+        const float lp2 = fmaxf(one_fma ? fmaf(f[i], p.k, -c_all) : fmaf(f[i] - st.x, p.k, -l2s),
+                                -1e30f);
         const float pr = ex2_approx(lp2);
-        float x = gl;
-        if (kEntropy) x = fmaf(ge, fmaf(lp2, 0.69314718f, h), x);
-        x = -pr * x;
-        f[i] = j0 + i == y && z != -INFINITY ? x + gl : x;
+        f[i] = pr * (kEntropy ? fmaf(x1, lp2, x0) : x0);
+      }
+      if (hit) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (at == static_cast<uint32_t>(i)) f[i] += gl;
       }
     } else {
 #pragma unroll
