@@ -291,9 +291,30 @@ struct Row {
     }
     return raw;
   }
+  // The 16 bytes from place j0 on, wherever they are aligned (-inf outside the row): the
+  // aligned words that hold them, shifted.
+  __device__ uint4 load_at(int j0) const {
+    if (j0 < 0 || j0 + kPer > V) {
+      uint4 raw = nothing();
+      T* e = reinterpret_cast<T*>(&raw);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (j0 + i >= 0 && j0 + i < V) e[i] = z[j0 + i];
+      return raw;
+    }
+    const uintptr_t at = reinterpret_cast<uintptr_t>(z + j0);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(at & ~uintptr_t{3});
+    if (kPer == 4 || (at & 2) == 0) return make_uint4(w[0], w[1], w[2], w[3]);
+    // (the first and last word hold places of the vector, so they may be read)
+    const uint32_t x[5] = {w[0], w[1], w[2], w[3], w[4]};
+    return make_uint4(__funnelshift_r(x[0], x[1], 16), __funnelshift_r(x[1], x[2], 16),
+                      __funnelshift_r(x[2], x[3], 16), __funnelshift_r(x[3], x[4], 16));
+  }
   // Bits of the allowed places of vector v (others of its bits are arbitrary).
-  __device__ uint32_t bits(int v) const {
-    const int j0 = v * kPer - shift, w = j0 >> 5, sh = j0 & 31;
+  __device__ uint32_t bits(int v) const { return bits_at(v * kPer - shift); }
+  // The same of the places from j0 on.
+  __device__ uint32_t bits_at(int j0) const {
+    const int w = j0 >> 5, sh = j0 & 31;
     const int last = (V - 1) >> 5;
     const uint32_t lo = w >= 0 && w <= last ? allowed[w] : 0u;
     const uint32_t hi = sh > 32 - kPer && w + 1 <= last ? allowed[w + 1] : 0u;
@@ -775,7 +796,7 @@ constexpr int kBwThreads = 256;
 constexpr int kBwVecs = 4;  // 16-byte vectors a thread
 
 // A block per piece of a row.  Vectors are those of the gradient's row; where the
-// logits' row starts elsewhere in its 16 bytes, they are read place by place.
+// logits' row starts elsewhere in its 16 bytes, they are read by words.
 template <typename T, bool kAllowed, bool kEntropy>
 __global__ void __launch_bounds__(kBwThreads) logits_backward_kernel(const BackwardArgs p) {
   constexpr int kPer = Logit<T>::kPer;
@@ -807,26 +828,31 @@ __global__ void __launch_bounds__(kBwThreads) logits_backward_kernel(const Backw
   const float l2s = st.y * kLog2e;
   uint4 raw[kBwVecs];
   uint32_t bits[kBwVecs];
+  const int b0 = piece * (kBwThreads * kBwVecs);  // the block's first vector
+  const bool whole = b0 * kPer >= shift && (b0 + kBwThreads * kBwVecs) * kPer <= shift + row.V;
+  if (live && same && whole) {  // every vector of the block is: no tests between the loads
+    const uint4* at = reinterpret_cast<const uint4*>(row.z - shift) + v0;
 #pragma unroll
-  for (int u = 0; u < kBwVecs; ++u) {
-    const int v = v0 + u * kBwThreads;
-    raw[u] = make_uint4(0, 0, 0, 0);
-    bits[u] = 0xffffffffu;
-    if (live && v < n_vec) {
-      const int j0 = v * kPer - shift;
-      if (same) {
-        raw[u] = row.load(v);
-        if (kAllowed) bits[u] = row.bits(v);
-      } else {
-        T* e = reinterpret_cast<T*>(&raw[u]);
-        uint32_t b = 0u;
+    for (int u = 0; u < kBwVecs; ++u) raw[u] = at[u * kBwThreads];
+    if (kAllowed) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          if (j0 + i >= 0 && j0 + i < row.V) {
-            e[i] = row.z[j0 + i];
-            if (kAllowed) b |= static_cast<uint32_t>(row.allows(j0 + i)) << i;
-          }
-        if (kAllowed) bits[u] = b;
+      for (int u = 0; u < kBwVecs; ++u) bits[u] = row.bits(v0 + u * kBwThreads);
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < kBwVecs; ++u) {
+      const int v = v0 + u * kBwThreads;
+      raw[u] = make_uint4(0, 0, 0, 0);
+      bits[u] = 0xffffffffu;
+      if (live && v < n_vec) {
+        const int j0 = v * kPer - shift;
+        if (same) {
+          raw[u] = row.load(v);
+          if (kAllowed) bits[u] = row.bits(v);
+        } else {
+          raw[u] = row.load_at(j0);
+          if (kAllowed) bits[u] = row.bits_at(j0);
+        }
       }
     }
   }

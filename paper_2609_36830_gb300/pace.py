@@ -212,6 +212,10 @@ _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 def _rows_arg(t, dtypes, shape, name: str):
     """(device pointer, row stride) of a 2-D tensor of one of `dtypes` whose rows are
     contiguous, of shape `shape` (None: any) on the current CUDA device."""
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() == _current_device()
+            and t.dtype in dtypes and t.is_contiguous() and t.dim() == 2
+            and (shape is None or t.shape == shape)):
+        return t.data_ptr(), t.shape[1]  # (as most are, in one chain)
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
     if not t.is_cuda or t.get_device() != _current_device():
