@@ -592,6 +592,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
     if (m != a.m) a = raised(a, ref, p.k);  // (the same for the warp)
     a.m = m;
     const float c_ref = ref * p.k;
+    float s = 0.0f, t = 0.0f;  // of this turn: long sums of small terms stay exact to 1e-7
     if (ordinary(c_ref)) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
@@ -603,8 +604,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
           float d = fmaf(f[i], p.k, -c_ref);
           if (!Logit<T>::kPacked) d = fmaxf(d, -FLT_MAX);
           const float e = ex2_approx(d);
-          a.s += e;
-          a.t = fmaf(e, d, a.t);
+          s += e;
+          t = fmaf(e, d, t);
         }
       }
     } else {
@@ -616,11 +617,13 @@ __global__ void __launch_bounds__(kMaxWarps * 32)
         for (int i = 0; i < kPer; ++i) {
           const float d = fmaxf((f[i] - ref) * p.k, -FLT_MAX);
           const float e = ex2_approx(d);
-          a.s += e;
-          a.t = fmaf(e, d, a.t);
+          s += e;
+          t = fmaf(e, d, t);
         }
       }
     }
+    a.s += s;
+    a.t += t;
   }
 
   // lanes, warps and CTAs: sums against the common maximum, added in a fixed order
