@@ -451,6 +451,7 @@ pace_status run_logprob_few(int64_t n_rows, const void* hidden, const void* w_vo
   a.H = H;
   a.V = V;
   a.n_tiles = (V + 2 * BM - 1) / (2 * BM);
+  temperature /= mma_sum_scale(H);
   a.scale_log2 = 1.4426950408889634f / temperature;
   a.targets = targets;
   a.rowidx = rowidx;

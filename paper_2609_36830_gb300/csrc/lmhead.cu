@@ -22,7 +22,8 @@
 //                     16 KB regions around the tile).  A block of more than 31 boxes is
 //                     fetched by four-row TMA gathers (tile::gather4), one per
 //                     lane.  No copy of the rows is made.
-//   warp 1 / lane 0   MMA issuer, even CTA only: tcgen05.mma.cta_group::2
+//   warp 1            MMA issuer, even CTA only (the warp runs whole and elects the
+//                     lane that issues): tcgen05.mma.cta_group::2
 //                     kind::f16 (bf16 x bf16 -> fp32), M=256 (128 rows from each
 //                     CTA), N=256 (128 vocabulary rows from each CTA), K=16 per
 //                     instruction; each CTA's tensor memory receives its own
@@ -1027,6 +1028,7 @@ pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* 
   if (few)
     return run_logprob_few(n_rows, hidden, w_vocab, targets, H, V, temperature, logprob, lse,
                            entropy, ws, n_valid_dev, rowidx, status_dev, st);
+  if (entropy) temperature /= mma_sum_scale(H);
   const int n_vtiles = (V + BN - 1) / BN;
   LmLaunch l;
   l.hidden = hidden;
