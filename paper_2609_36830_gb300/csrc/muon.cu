@@ -83,6 +83,10 @@ struct NsArgs {
   __half* a;
   int split;               // parts that X X^T's tiles are split into along l
   float* part;             // [tile][part][64 blocks][32 columns][32 rows], or null
+  int slices;              // pairs that share a matrix of at most 256 rows (columns if tall)
+  int direct;              // each CTA adds up its rows of A itself, from one of two buffers
+  float* slice_part;       // [batch][slices][blocks][32 columns][32 rows] of X X^T, 1 + direct times
+  float* slice_sum;        // [batch][slices] squares of U
   float ca, cb, cc;        // the coefficients
   float sx, sa, sc;        // powers of two: X, A and C are held times these
   unsigned* ctr;           // arrivals at the grid barriers, zero at launch
@@ -346,18 +350,26 @@ __device__ __forceinline__ void store_result1(const NsArgs& p, const Block& b, i
                                               const float* tile) {
   const int64_t col = b.col0 + lane;
   if (col >= b.cols) return;
-#pragma unroll 4
-  for (int r = 0; r < 32; ++r) {
-    const int64_t row = b.row0 + r;
-    if (row >= b.rows) break;
-    const float o = tile[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
+  constexpr int kRows = 8;  // loads before stores: a load does not pass one that may be to its place
+#pragma unroll 1
+  for (int r0 = 0; r0 < 32; r0 += kRows) {
+    const int64_t row0 = b.row0 + r0, at = (b.z * b.rows + row0) * b.cols + col;
+    float w[kRows];
     if (p.weight) {
-      const int64_t at = (b.z * b.rows + row) * b.cols + col;
-      const float v = fmaf(p.weight[at], p.keep, -p.rate * o);
-      p.weight[at] = v;
-      if (p.weight16) p.weight16[at] = __float2bfloat16_rn(v);
-    } else {
-      p.out[b.z * p.out_bs + row * p.out_ld + col] = __float2bfloat16_rn(o);
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) w[r] = row0 + r < b.rows ? p.weight[at + r * b.cols] : 0.0f;
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      if (row0 + r >= b.rows) return;
+      const float o = tile[(r0 + r) * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
+      if (p.weight) {
+        const float v = fmaf(w[r], p.keep, -p.rate * o);
+        p.weight[at + r * b.cols] = v;
+        if (p.weight16) p.weight16[at + r * b.cols] = __float2bfloat16_rn(v);
+      } else {
+        p.out[b.z * p.out_bs + (row0 + r) * p.out_ld + col] = __float2bfloat16_rn(o);
+      }
     }
   }
 }
@@ -958,11 +970,15 @@ __global__ void __launch_bounds__(kElemThreads, 4) direction_kernel(const UArgs 
   }
 }
 
-// ------------------------------------------------------------- matrices up to 256 x 256
+// ------------------------------------------------- matrices whose shorter side is up to 256
 
 // One CTA pair does everything for a matrix of at most 256 x 256, in shared memory and
 // without a grid barrier: norm, all products, result.  (The phases of
 // newton_schulz_kernel spend 4-5 us each in barrier, loads and stores whatever the size.)
+// A longer X is cut into slices of 256 columns, a pair each: C X needs no other slice, and
+// X X^T is the sum of the slices' products.  The pairs of a matrix meet twice a step: every
+// pair leaves its product in float32, each CTA adds up its share of them, in the order of the
+// slices, and every CTA reads the rows of A that it needs.
 // X is s x l with s <= l, so a tall U is transposed as it is read.  Operands lie in the
 // layouts that the TMA would build (128-byte swizzle), 64 KB each in a CTA:
 //   rows     the CTA's 128 rows of X, and of C: [K block][128 rows][64], K-major.  They are
@@ -971,15 +987,17 @@ __global__ void __launch_bounds__(kElemThreads, 4) direction_kernel(const UArgs 
 //   gram     the same of A;
 //   columns  the CTA's 128 columns of X: [K block][64-column box][64 rows of X][64],
 //            MN-major, the B operand of C X.
-// C takes the place of the rows of X once X X^T is done; a step's result goes to the CTA's
-// own rows and to the columns of either CTA.
-constexpr int kSmallWarps = 16;  // four for each quarter of the rows, 64 columns each
+// C takes the place of the rows of X once X X^T is done, and a step's rows that of A; its
+// columns go to the CTA that has them.  A product comes in two halves of 128 columns, the
+// first 64 of either CTA's part of B and then the others, and the first leaves the
+// accumulator while the second is computed, which does not read what that writes.
+constexpr int kSmallWarps = 16;  // four for each quarter of the rows, 2 x 32 columns each
 constexpr int kSmallThreads = 32 * kSmallWarps;
-constexpr int kSmallCols = 64;
 constexpr uint32_t kRegion = 65536;
 constexpr size_t kSmallSmem = 1024 + 3 * kRegion + 256;
 constexpr int kSmallSide = 256;
 
+template <bool kSliced>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
     newton_schulz_small_kernel(const __grid_constant__ UArgs u, const __grid_constant__ NsArgs p) {
   extern __shared__ unsigned char smem_raw[];
@@ -988,20 +1006,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
   unsigned char* rows_at = smem;
   unsigned char* gram_at = smem + kRegion;
   unsigned char* cols_at = smem + 2 * kRegion;
-  uint64_t* done = reinterpret_cast<uint64_t*>(smem + 3 * kRegion);  // a product is complete
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  uint64_t* done = reinterpret_cast<uint64_t*>(smem + 3 * kRegion);  // [2] a product's halves
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* pair_sum = reinterpret_cast<float*>(tmem_slot + 2);   // [2] the CTAs' squares
   float* warp_sum = pair_sum + 2;                              // [kSmallWarps]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t crank = cluster_ctarank();
-  const int z = static_cast<int>(blockIdx.x) / 2;
-  const int s = static_cast<int>(p.s), l = static_cast<int>(p.l);
+  const int z = static_cast<int>(blockIdx.x) / (kSliced ? 2 * p.slices : 2);
+  const int slice = kSliced ? static_cast<int>(blockIdx.x) / 2 - z * p.slices : 0;
+  const int l0 = slice * kSmallSide;  // first column of X here
+  const int s = static_cast<int>(p.s);
+  const int l = min(static_cast<int>(p.l) - l0, kSmallSide);  // columns here
   const int ks = (s + BK - 1) / BK, kl = (l + BK - 1) / BK;  // K blocks of either side
 
   if (threadIdx.x == 0) {
-    mbar_init(done, 1);
+    mbar_init(&done[0], 1);
+    mbar_init(&done[1], 1);
     *abort_flag = 0;
     fence_barrier_init();
   }
@@ -1015,41 +1037,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  // Thread of the epilogue: row of X, and 64 of its columns, which CTA `owner` has as columns.
-  const int quad = warp & 3, c_begin = (warp >> 2) * kSmallCols;
-  const uint32_t owner = static_cast<uint32_t>(c_begin / BM);
+  // Thread of the epilogue: row of X, and its columns c_begin ... + 31 of a first half and
+  // c_begin + 64 ... of the second, which CTA `owner` has as columns.
+  const int quad = warp & 3;
+  const uint32_t owner = static_cast<uint32_t>(warp) >> 3;
+  const int c_begin = static_cast<int>(owner) * BM + (warp >> 2 & 1) * 32;
   const int row_l = quad * 32 + lane;
   const int row = static_cast<int>(crank) * BM + row_l;
-  // U's values at 32 columns of the thread's row (zeros outside); the momentum is updated
-  auto load_u = [&](int col0, float (&v)[32]) {
-    if (!p.tall && u.vec && row < s) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (col0 + 8 * q < l) direction8<true>(u, z, row, col0 + 8 * q, f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[8 * q + i] = f[i];
-      }
-      return;
-    }
-    // X[row][col] is U[col][row] of a tall U: a warp's lanes read one of its rows
-    const int64_t ur = p.tall ? col0 : row, uc = p.tall ? row : col0;
-    const int64_t g_at = z * u.bs + ur * u.ld + uc, g_step = p.tall ? u.ld : 1;
-    const int64_t m_at = (z * u.rows + ur) * u.cols + uc, m_step = p.tall ? u.cols : 1;
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      v[i] = row < s && col0 + i < l ? load1(u, g_at + i * g_step) : 0.0f;
-    if (u.momentum) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        if (row >= s || col0 + i >= l) continue;
-        float* mp = u.momentum + m_at + i * m_step;
-        const float m = fmaf(u.mu, *mp, v[i]);
-        *mp = m;
-        v[i] = direction(u, v[i], m);
-      }
-    }
-  };
   // 32 columns of a row in a K-major region
   auto put_rows = [&](unsigned char* region, int col0, const uint32_t (&h)[16]) {
     unsigned char* at = region + (col0 >> 6) * 16384 + row_l * 128;
@@ -1079,18 +1073,185 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
     }
   };
 
-  // The norm: squares of the thread, the warp, the CTA, the pair.
-  float first[2][32];  // the thread's columns of U
+  // The matrix's CTAs wait for each other.  After an abort they only arrive.
+  unsigned* const ctr = p.ctr + z;
+  unsigned target = 0;
+  auto meet = [&]() {
+    target += 2u * static_cast<unsigned>(p.slices);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      red_release(ctr);
+      if (!*abort_flag && !wait_phase(ctr, target, abort_flag)) {
+        if (!*abort_flag) report(p.status, PACE_ERR_TIMEOUT);
+        *abort_flag = 1;
+      }
+    }
+    __syncthreads();
+  };
+  // X X^T in blocks of 32 x 32: [4 columns][row][4]
+  const int nb = (s + 31) / 32;
+  const int n_quads = nb * nb * 256;  // of four columns of a row
+  const int64_t buffer = static_cast<int64_t>(p.batch) * p.slices * n_quads * 4;
+  auto add_slices = [&](float f) {  // this CTA's share of A
+    // 32 / groups quads a warp; its groups of lanes take every groups-th slice
+    const int groups = p.slices >= 32 ? 8 : p.slices >= 16 ? 4 : p.slices >= 8 ? 2 : 1;
+    const int per = 32 / groups, g = lane / per, n_units = n_quads / per;
+    const int n_warps = 2 * p.slices * kSmallWarps;
+    const float4* const at = reinterpret_cast<const float4*>(p.slice_part) +
+                             static_cast<int64_t>(z) * p.slices * n_quads + lane % per;
+    constexpr int kUnits = 4, kDeep = 4;  // loads in flight
+    for (int u0 = (2 * slice + static_cast<int>(crank)) * kSmallWarps + warp; u0 < n_units;
+         u0 += kUnits * n_warps) {
+      float4 sum[kUnits];
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j) sum[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int k0 = g; k0 < p.slices + g; k0 += kDeep * groups) {
+        float4 x[kDeep][kUnits];
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i)
+#pragma unroll
+          for (int j = 0; j < kUnits; ++j) {
+            const int k = k0 + i * groups, unit = u0 + j * n_warps;
+            x[i][j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (k < p.slices && unit < n_units)
+              x[i][j] = __ldcg(at + static_cast<int64_t>(k) * n_quads + unit * per);
+          }
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i)
+#pragma unroll
+          for (int j = 0; j < kUnits; ++j) {
+            sum[j].x += x[i][j].x, sum[j].y += x[i][j].y;
+            sum[j].z += x[i][j].z, sum[j].w += x[i][j].w;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j) {
+        for (int x = per; x < 32; x <<= 1) {
+          sum[j].x += __shfl_xor_sync(0xffffffffu, sum[j].x, x);
+          sum[j].y += __shfl_xor_sync(0xffffffffu, sum[j].y, x);
+          sum[j].z += __shfl_xor_sync(0xffffffffu, sum[j].z, x);
+          sum[j].w += __shfl_xor_sync(0xffffffffu, sum[j].w, x);
+        }
+        const int unit = u0 + j * n_warps, quad_no = unit * per + lane % per;
+        if (unit >= n_units || g != 0) continue;
+        const int block = quad_no >> 8, in = quad_no & 255;
+        const int a_row = (block / nb) * 32 + (in & 31), a_col = (block % nb) * 32 + 4 * (in >> 5);
+        if (a_row < s)
+          *reinterpret_cast<uint2*>(p.a + (static_cast<int64_t>(z) * s + a_row) * p.lda + a_col) =
+              make_uint2(half2_rn(sum[j].x * f, sum[j].y * f), half2_rn(sum[j].z * f, sum[j].w * f));
+      }
+    }
+  };
+  auto read_gram = [&]() {  // the CTA's rows of A, added up by all: four threads a row
+    const int r = static_cast<int>(threadIdx.x) >> 2, a_row = static_cast<int>(crank) * BM + r;
+    const __half* const at = p.a + (static_cast<int64_t>(z) * s + a_row) * p.lda;
+    uint4 w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int q = (threadIdx.x & 3) + 4 * j;  // eight columns
+      w[j] = make_uint4(0u, 0u, 0u, 0u);
+      if (a_row < s && 8 * q < 32 * nb) w[j] = __ldcg(reinterpret_cast<const uint4*>(at + 8 * q));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int q = (threadIdx.x & 3) + 4 * j;
+      if (q < ks * 8)
+        *reinterpret_cast<uint4*>(gram_at + (q >> 3) * 16384 + r * 128 +
+                                  (((q & 7) ^ (r & 7)) << 4)) = w[j];
+    }
+  };
+  auto add_rows = [&](const float* part, float f) {  // the CTA's rows of A from the products
+#pragma unroll 1
+    for (int c = c_begin; c < ks * BK && c < c_begin + 128; c += 64) {
+      float v[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+      if (row - lane < s && c < s) {
+        const float4* at = reinterpret_cast<const float4*>(part) +
+                           static_cast<int64_t>(z) * p.slices * n_quads +
+                           ((row >> 5) * nb + (c >> 5)) * 256 + lane;
+#pragma unroll 1
+        for (int k = 0; k < p.slices; k += 2, at += 2 * n_quads) {
+          const bool two = k + 1 < p.slices;
+          float4 x[8], y[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) x[q] = __ldcg(at + 32 * q);
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            y[q] = two ? __ldcg(at + n_quads + 32 * q) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            v[4 * q] += x[q].x + y[q].x;
+            v[4 * q + 1] += x[q].y + y[q].y;
+            v[4 * q + 2] += x[q].z + y[q].z;
+            v[4 * q + 3] += x[q].w + y[q].w;
+          }
+        }
+      }
+      uint32_t h[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i] * f, v[2 * i + 1] * f);
+      put_rows(gram_at, c, h);
+    }
+  };
+
+  // where a half product's column lies in the accumulator
+  auto acc_column = [](int c) { return (c & 64) * 2 + (c & 63) + (c >> 7) * 64; };
+
+  // The norm: squares of the thread, the warp, the CTA, the pair, the slices.
+  // A block of 32 x 32 goes through a tile of the warp's, so that lanes take U's columns
+  // whether they are columns of X or (of a tall U) rows.  All loads come before the stores: a
+  // load does not pass a store that may be to its place.
+  struct Place {
+    int64_t row, col;  // of U, for the lane's first value; the others lie in the rows below
+    int n;
+  };
+  auto place = [&](int c) {
+    const int r0 = row - lane;
+    Place q;
+    q.row = p.tall ? l0 + c : r0;
+    q.col = p.tall ? row : l0 + c + lane;
+    q.n = p.tall ? (row < s ? l - c : 0) : (c + lane < l ? s - r0 : 0);
+    return q;
+  };
+  auto tile_put = [&](float* tile, const float (&v)[32]) {  // value i of a lane, as in place()
+#pragma unroll
+    for (int i = 0; i < 32; ++i) tile[p.tall ? lane * 32 + (i ^ lane) : i * 32 + (lane ^ i)] = v[i];
+  };
+  float* const tiles = reinterpret_cast<float*>(gram_at) + warp * 2048;  // A's place, the columns'
   float ss = 0.0f;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) load_u(c_begin + 32 * k, first[k]);
-#pragma unroll
+#pragma unroll 1
   for (int k = 0; k < 2; ++k) {
+    const Place q = place(c_begin + 64 * k);
+    float v[32], m[32];
+    const int64_t at = z * u.bs + q.row * u.ld + q.col;
+    if (u.is_bf16) {
+      const __nv_bfloat16* const g = static_cast<const __nv_bfloat16*>(u.g) + at;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = i < q.n ? __bfloat162float(g[i * u.ld]) : 0.0f;
+    } else {
+      const float* const g = static_cast<const float*>(u.g) + at;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = i < q.n ? g[i * u.ld] : 0.0f;
+    }
+    if (u.momentum) {
+      float* const mp = u.momentum + (z * u.rows + q.row) * u.cols + q.col;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) m[i] = i < q.n ? mp[i * u.cols] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        m[i] = fmaf(u.mu, m[i], v[i]);
+        if (i < q.n) mp[i * u.cols] = m[i];
+        v[i] = direction(u, v[i], m[i]);
+      }
+    }
     float part = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) part = fmaf(first[k][i], first[k][i], part);
+    for (int i = 0; i < 32; ++i) part = fmaf(v[i], v[i], part);
     ss += part;
+    tile_put(tiles + k * 1024, v);
   }
+  __syncwarp();
 #pragma unroll
   for (int x = 16; x > 0; x >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, x);
   if (lane == 0) warp_sum[warp] = ss;
@@ -1101,19 +1262,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
     st_cluster_u32(cluster_addr(&pair_sum[crank], threadIdx.x), __float_as_uint(sum));
   }
   cluster_sync();
-  const float norm = sqrtf(pair_sum[0] + pair_sum[1]);
+  float squares = pair_sum[0] + pair_sum[1];
+  if (kSliced) {
+    if (crank == 0 && threadIdx.x == 0) p.slice_sum[z * p.slices + slice] = squares;
+    meet();
+    squares = 0.0f;
+    for (int k = lane; k < p.slices; k += 32) squares += __ldcg(p.slice_sum + z * p.slices + k);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, x);
+  }
+  const float norm = sqrtf(squares);
   const float scale = p.sx / (norm + u.eps);
-  if (!(norm < INFINITY) && crank == 0 && threadIdx.x == 0) report(p.status, PACE_ERR_NAN_INPUT);
+  if (!(norm < INFINITY) && slice == 0 && crank == 0 && threadIdx.x == 0)
+    report(p.status, PACE_ERR_NAN_INPUT);
+  uint32_t first[2][16];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const int c = c_begin + 32 * k;
-    if (c >= kl * BK) break;
-    uint32_t h[16];
+    const float* const tile = tiles + k * 1024 + lane * 32;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      h[i] = half2_rn(first[k][2 * i] * scale, first[k][2 * i + 1] * scale);
-    put_rows(rows_at, c, h);
-    put_columns(c, h);
+      first[k][i] = half2_rn(tile[(2 * i) ^ lane] * scale, tile[(2 * i + 1) ^ lane] * scale);
+  }
+  cluster_sync();  // the columns' place is free in both CTAs
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c = c_begin + 64 * k;
+    if (c >= kl * BK) break;
+    put_rows(rows_at, c, first[k]);
+    put_columns(c, first[k]);
   }
 
   bool ok = true;
@@ -1131,28 +1307,67 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
         const uint32_t a_at = smem_u32(kind == kPoly ? gram_at : rows_at);
         const uint32_t b_at = smem_u32(kind == kStep ? cols_at : kind == kPoly ? gram_at : rows_at);
         const bool b_mn = kind == kStep;
-        const uint32_t idesc = idesc_f16(TM, false, b_mn);
+        const uint32_t idesc = idesc_f16(BM, false, b_mn);
         const int nkb = kind == kGram ? kl : ks;
-        for (int kb = 0; kb < nkb; ++kb) {
-          const uint64_t a = operand_desc(a_at + kb * 16384, false);
-          const uint64_t b = operand_desc(b_at + kb * 16384, b_mn);
+        for (int h = 0; h < 2; ++h) {
+          if (h == 0 || (b_mn ? l : s) > BK) {  // (nothing is in the second half otherwise)
+            for (int kb = 0; kb < nkb; ++kb) {
+              const uint64_t a = operand_desc(a_at + kb * 16384, false);
+              const uint64_t b = operand_desc(b_at + kb * 16384 + h * 8192, b_mn);
 #pragma unroll
-          for (int k = 0; k < BK / 16; ++k)
-            tc_mma_f16_pair(tmem, a + k * 2, b + k * (b_mn ? 128 : 2), idesc,
-                            (kb > 0 || k > 0) ? 1u : 0u);
+              for (int k = 0; k < BK / 16; ++k)
+                tc_mma_f16_pair(tmem + h * BM, a + k * 2, b + k * (b_mn ? 128 : 2), idesc,
+                                (kb > 0 || k > 0) ? 1u : 0u);
+            }
+          }
+          tc_commit_both(&done[h]);
         }
-        tc_commit_both(done);
       }
       __syncwarp();
     }
-    if (ok && !__all_sync(0xffffffffu, mbar_wait_bounded(done, ph & 1, abort_flag))) {
-      if (!*abort_flag) report(p.status, PACE_ERR_TIMEOUT);
-      *abort_flag = 1;
-      ok = false;
-    }
-    if (!ok) continue;  // the barriers go on
-    tc_fence_after();
+    auto wait_half = [&](int h) {
+      if (ok && !__all_sync(0xffffffffu, mbar_wait_bounded(&done[h], ph & 1, abort_flag))) {
+        if (!*abort_flag) report(p.status, PACE_ERR_TIMEOUT);
+        *abort_flag = 1;
+        ok = false;
+      }
+      if (ok) tc_fence_after();
+      return ok;
+    };
     const uint32_t tbase = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    if (kSliced && kind == kGram) {
+      // (two buffers: a CTA may still read one while another writes the next step's)
+      float* const part = p.slice_part + (p.direct && (ph / 3 & 1) ? buffer : 0);
+      const float f = p.sa / (p.sx * p.sx);
+      float4* const at = reinterpret_cast<float4*>(part) +
+                         ((static_cast<int64_t>(z) * p.slices + slice) * nb + (row >> 5)) * nb * 256 +
+                         lane;
+#pragma unroll 1
+      for (int h = 0; h < 2 && wait_half(h); ++h) {
+        const int c = c_begin + 64 * h;
+        if (row - lane >= s || c >= s) continue;
+        float v[32];
+        tmem_ld_32x32b_x32(tbase + acc_column(c), v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          __stcg(at + (c >> 5) * 256 + 32 * q,
+                 make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
+      }
+      meet();
+      if (!p.direct) {
+        if (ok) add_slices(f);
+        meet();
+      }
+      if (*abort_flag) ok = false;
+      if (ok) {
+        if (p.direct)
+          add_rows(part, f);
+        else
+          read_gram();
+      }
+      continue;
+    }
     float f_acc, f_src = 0.0f, diag = 0.0f;
     if (kind == kGram) {
       f_acc = p.sa / (p.sx * p.sx);
@@ -1166,9 +1381,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
     const int width = last ? l : (kind == kStep ? kl : ks) * BK;
     // (not unrolled: a quarter of the kernel's stalls are instructions on their way)
 #pragma unroll 1
-    for (int c = c_begin; c < c_begin + kSmallCols && c < width; c += 32) {
+    for (int half = 0; half < 2 && wait_half(half); ++half) {  // (else the barriers go on)
+      const int c = c_begin + 64 * half;
+      if (c >= width) continue;
       float v[32];
-      tmem_ld_32x32b_x32(tbase + c, v);
+      tmem_ld_32x32b_x32(tbase + acc_column(c), v);
       tmem_wait_ld();
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] *= f_acc;
@@ -1197,37 +1414,52 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmallThreads, 1)
         uint32_t h[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) h[i] = half2_rn(v[2 * i], v[2 * i + 1]);
-        put_rows(kind == kGram ? gram_at : rows_at, c, h);
+        put_rows(kind == kPoly ? rows_at : gram_at, c, h);
         if (kind == kStep) put_columns(c, h);
-      } else if (p.tall) {  // rows of X are columns of the result: whole lines as they are
+      } else {  // the result, to tiles in A's place and, the tensor cores being done, in C's
+        float* const tile = reinterpret_cast<float*>(half == 0 ? gram_at : rows_at) + warp * 1024;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          if (row >= s || c + i >= l) continue;
-          if (p.weight) {
-            const int64_t at = (static_cast<int64_t>(z) * l + c + i) * s + row;
-            const float w = fmaf(p.weight[at], p.keep, -p.rate * v[i]);
-            p.weight[at] = w;
-            if (p.weight16) p.weight16[at] = __float2bfloat16_rn(w);
-          } else {
-            p.out[z * p.out_bs + (c + i) * p.out_ld + row] = __float2bfloat16_rn(v[i]);
-          }
-        }
-      } else {  // through shared memory (A is not needed any more)
-        float* tile = reinterpret_cast<float*>(gram_at + warp * 4096);
-        const Block b{row - lane, s, c, l, z};
-        float4 w[8];
-        if (p.vec && p.weight) load_weights(p, b, lane, w);
-        __syncwarp();
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-          *reinterpret_cast<float4*>(tile + lane * 32 + ((q ^ (lane & 7)) << 2)) =
-              make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-        __syncwarp();
-        if (p.vec)
-          store_result4(p, b, lane, tile, w);
-        else
-          store_result1(p, b, lane, tile);
+        for (int i = 0; i < 32; ++i) tile[lane * 32 + (i ^ lane)] = v[i];
       }
+    }
+    if (kind == kStep) {
+      unsigned char* const x_at = gram_at;
+      gram_at = rows_at;
+      rows_at = x_at;
+    }
+  }
+
+  // The result goes out as U came in.  (Outside the loop, whose instructions the SM then
+  // keeps: with this inside, the loop took 62 us instead of 46.)
+  __syncwarp();
+#pragma unroll 1
+  for (int k = 0; ok && k < 2; ++k) {
+    const Place q = place(c_begin + 64 * k);
+    // (rows and A have changed places after the last step)
+    const float* const tile = reinterpret_cast<const float*>(k == 0 ? rows_at : gram_at) + warp * 1024;
+    float v[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = tile[p.tall ? lane * 32 + (i ^ lane) : i * 32 + (lane ^ i)];
+    if (p.weight) {
+      const int64_t cols = u.cols, at = (z * u.rows + q.row) * cols + q.col;
+      float w[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) w[i] = i < q.n ? p.weight[at + i * cols] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        w[i] = fmaf(w[i], p.keep, -p.rate * v[i]);
+        if (i < q.n) p.weight[at + i * cols] = w[i];
+      }
+      if (p.weight16) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (i < q.n) p.weight16[at + i * cols] = __float2bfloat16_rn(w[i]);
+      }
+    } else {
+      __nv_bfloat16* const o = p.out + z * p.out_bs + q.row * p.out_ld + q.col;
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i < q.n) o[i * p.out_ld] = __float2bfloat16_rn(v[i]);
     }
   }
 
@@ -1245,9 +1477,25 @@ struct MuonWs {
   float* partial;
   float* part;   // X X^T in parts
   int split;
-  unsigned* ctr;
+  int slices;  // of X's columns, for newton_schulz_small_kernel; 0: not for it
+  int direct;
+  float *slice_part, *slice_sum;
+  unsigned* ctr;  // [1], or [batch] for slices
   int64_t ldx, lda;
 };
+
+// Slices of a matrix's longer side whose pairs can all be on the device (the rule goes by
+// kMaxClusters, so that the workspace does not depend on the device).
+int slice_count(int64_t batch, int64_t s, int64_t l) {
+  if (s > kSmallSide || batch < 1) return 0;
+  const int64_t n = (l + kSmallSide - 1) / kSmallSide;
+  return n == 1 || batch * n <= kMaxClusters ? static_cast<int>(n) : 0;
+}
+
+// Whether every CTA adds up its rows of A by itself, which saves a meeting and takes a read of
+// all slices' products: up to 6 slices (256 x 512 103 -> 85 us, 256 x 1,536 99 -> 97, 256 x 2,048
+// 101 -> 105), 8 of 64 rows (64 x 2,048 74 -> 69, 64 x 8,192 79 -> 93).
+int add_directly(int slices, int64_t s) { return slices <= (s <= 64 ? 8 : 6) ? 1 : 0; }
 
 void carve_muon_ws(Carver& cv, int64_t batch, int64_t rows, int64_t cols, MuonWs* w) {
   const int64_t s = rows < cols ? rows : cols;
@@ -1259,10 +1507,19 @@ void carve_muon_ws(Carver& cv, int64_t batch, int64_t rows, int64_t cols, MuonWs
   w->a = cv.take<__half>(na);
   w->c = cv.take<__half>(na);
   w->partial = cv.take<float>(static_cast<size_t>(batch) * elem_blocks(batch > 0 ? batch : 1, rows, cols));
-  w->ctr = cv.take<unsigned>(1);
+  w->ctr = cv.take<unsigned>(static_cast<size_t>(batch > 0 && batch < kMaxClusters ? batch : 1));
   const int64_t tiles = batch * sym_tiles(s);
   w->split = tiles > 0 ? gram_split(tiles, rows < cols ? cols : rows) : 1;
   w->part = w->split > 1 ? cv.take<float>(static_cast<size_t>(tiles) * w->split * TM * TM) : nullptr;
+  w->slices = slice_count(batch, s, rows < cols ? cols : rows);
+  w->slice_part = w->slice_sum = nullptr;
+  w->direct = 0;
+  if (w->slices > 1) {
+    const size_t pairs = static_cast<size_t>(batch) * w->slices, nb = (s + 31) / 32;
+    w->direct = add_directly(w->slices, s);
+    w->slice_part = cv.take<float>((1 + w->direct) * pairs * nb * nb * 1024);
+    w->slice_sum = cv.take<float>(pairs);
+  }
 }
 
 // The largest |a x + b x^3 + c x^5| over 0 <= x <= r.
@@ -1311,22 +1568,23 @@ bool choose_scales(const PaceMuonParams* q, NsArgs* p) {
   return true;
 }
 
-pace_status ns_max_clusters(int* out) {
+// Pairs of `kernel` that the device holds at once, at most kMaxClusters; its shared memory is
+// opted into on the way.
+template <typename Kernel>
+pace_status max_clusters_of(Kernel* kernel, int threads, size_t smem, int* cache, int* out) {
   constexpr int kMaxDevices = 64;
-  static int cached[kMaxDevices];
   static std::mutex mu;
   int dev = 0;
   PACE_TRY_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= kMaxDevices) return PACE_ERR_CUDA;
   std::lock_guard<std::mutex> g(mu);
-  if (cached[dev] == 0) {
-    PACE_TRY_CUDA(cudaFuncSetAttribute(newton_schulz_kernel,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(kSmemBytes)));
+  if (cache[dev] == 0) {
+    PACE_TRY_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(smem)));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(sm_count()) & ~1u, 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
+    cfg.dynamicSmemBytes = smem;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2;
@@ -1335,32 +1593,42 @@ pace_status ns_max_clusters(int* out) {
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     int n = 0;
-    PACE_TRY_CUDA(cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel, &cfg));
+    PACE_TRY_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
     if (n < 1) return PACE_ERR_CUDA;
-    cached[dev] = n < kMaxClusters ? n : kMaxClusters;
+    cache[dev] = n < kMaxClusters ? n : kMaxClusters;
   }
-  *out = cached[dev];
+  *out = cache[dev];
   return PACE_OK;
 }
 
-pace_status launch_small(const UArgs& u, const NsArgs& n, int64_t batch, cudaStream_t st) {
-  constexpr int kMaxDevices = 64;
-  static bool done[kMaxDevices] = {};  // shared-memory opt-in made on that device
-  static std::mutex mu;
-  int dev = 0;
-  PACE_TRY_CUDA(cudaGetDevice(&dev));
-  if (dev < 0 || dev >= kMaxDevices) return PACE_ERR_CUDA;
-  {
-    std::lock_guard<std::mutex> g(mu);
-    if (!done[dev]) {
-      PACE_TRY_CUDA(cudaFuncSetAttribute(newton_schulz_small_kernel,
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         static_cast<int>(kSmallSmem)));
-      done[dev] = true;
-    }
+pace_status ns_max_clusters(int* out) {
+  static int cache[64];
+  return max_clusters_of(newton_schulz_kernel, kThreads, kSmemBytes, cache, out);
+}
+
+pace_status small_max_clusters(int* out) {
+  static int cache[64];
+  return max_clusters_of(newton_schulz_small_kernel<true>, kSmallThreads, kSmallSmem, cache, out);
+}
+
+// A cooperative launch if the kernel's CTAs wait for each other: all are resident then.
+template <typename Kernel, typename... Args>
+pace_status launch_pairs(Kernel* kernel, int64_t pairs, int threads, size_t smem, bool together,
+                         cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs), 1, 1);
+  cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = together ? 1 : 0;
+  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return PACE_ERR_CUDA;
   }
-  newton_schulz_small_kernel<<<static_cast<unsigned>(2 * batch), kSmallThreads, kSmallSmem, st>>>(
-      u, n);
   return last_launch_status();
 }
 
@@ -1411,7 +1679,27 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
   n.split = w.split;
   n.part = w.part;
 
-  if (n.l <= kSmallSide) return launch_small(u, n, batch, st);
+  if (w.slices == 1) {
+    int most = 0;  // (any number of pairs: none waits for another)
+    static int cache[64];
+    PACE_TRY(max_clusters_of(newton_schulz_small_kernel<false>, kSmallThreads, kSmallSmem, cache,
+                             &most));
+    return launch_pairs(newton_schulz_small_kernel<false>, batch, kSmallThreads, kSmallSmem, false,
+                        st, u, n);
+  }
+  if (w.slices > 1) {
+    int most = 0;
+    PACE_TRY(small_max_clusters(&most));
+    if (batch * w.slices <= most) {
+      n.slices = w.slices;
+      n.slice_part = w.slice_part;
+      n.direct = w.direct;
+      n.slice_sum = w.slice_sum;
+      PACE_TRY_CUDA(cudaMemsetAsync(w.ctr, 0, static_cast<size_t>(batch) * sizeof(unsigned), st));
+      return launch_pairs(newton_schulz_small_kernel<true>, batch * w.slices, kSmallThreads,
+                          kSmallSmem, true, st, u, n);
+    }
+  }
   Maps m;
   const int64_t xbs = u.rows * w.ldx, cbs = n.s * w.lda;
   for (int i = 0; i < 2; ++i) {
@@ -1444,21 +1732,7 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
   int64_t pairs = 2 * batch * step_tiles(n.s, n.l);
   if (batch * sym_tiles(n.s) * n.split > pairs) pairs = batch * sym_tiles(n.s) * n.split;
   const int64_t clusters = pairs < max_clusters ? pairs : max_clusters;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(2 * clusters), 1, 1);
-  cfg.blockDim = dim3(kThreads, 1, 1);
-  cfg.dynamicSmemBytes = kSmemBytes;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeCooperative;  // every CTA is resident: the barriers' waits end
-  attr[0].val.cooperative = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, newton_schulz_kernel, m, n) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return PACE_ERR_CUDA;
-  }
-  return last_launch_status();
+  return launch_pairs(newton_schulz_kernel, clusters, kThreads, kSmemBytes, true, st, m, n);
 }
 
 }  // namespace

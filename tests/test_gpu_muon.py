@@ -170,6 +170,44 @@ def test_nan_is_reported():
         check(got[0], steps64(u[0]))  # the other matrix is not touched by it
 
 
+@pytest.mark.parametrize("b,m,n", [
+    (1, 34, 572), (2, 84, 4891), (6, 2825, 166), (1, 256, 14336), (1, 2528, 114), (1, 129, 512),
+    (1, 512, 256), (1, 40, 19456), (1, 40, 19457), (38, 20, 300), (39, 300, 20), (1, 256, 769),
+    (2, 4097, 33), (9, 200, 2049)])
+def test_one_short_side(b, m, n):
+    """Slices of 256 of the longer side, and stacks that have too many of them."""
+    u = gauss(b, m, n, strong=max(1, min(m, n) // 16))
+    status = pace.new_status(DEV)
+    got = pace.orthogonalize(u, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    check(got, steps64(u))
+    assert torch.equal(pace.orthogonalize(u), got)
+
+
+def test_short_side_in_a_graph_in_place_and_with_nan():
+    u = gauss(3, 90, 1500, dtype=torch.bfloat16)
+    want = pace.orthogonalize(u)
+    ws = pace.workspace(pace.muon_workspace_size(3, 90, 1500), DEV)
+    out = torch.zeros_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pace.orthogonalize(u, out=out, ws=ws)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    bad = u.clone()
+    bad[1, 50, 1400] = math.nan
+    status = pace.new_status(DEV)
+    got = pace.orthogonalize(bad, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == pace.ERR_NAN_INPUT
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+    assert torch.equal(pace.orthogonalize(u, out=u), want)
+
+
 # ---------------------------------------------------------------- the weight update
 
 @pytest.mark.parametrize("gdtype", [torch.float32, torch.bfloat16])
@@ -197,6 +235,12 @@ def test_muon_update(shape, nesterov, gdtype):
             shape[-1] * shape[-2])
         assert ((w.double() - w64).abs() <= 6 * noise + 2.0 ** -22 * w64.abs()).all()
         assert torch.equal(copy, w.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("shape", [(105, 42), (42, 105), (2, 700, 130), (100, 1000), (104, 515)])
+def test_muon_update_with_a_short_side(shape):
+    test_muon_update(shape, True, torch.float32)
+    test_muon_update(shape, False, torch.bfloat16)
 
 
 def test_update_of_unaligned_tensors():
