@@ -862,16 +862,19 @@ __device__ __forceinline__ void direction8(const UArgs& p, int z, int64_t row, i
     }
     return;
   }
+  // (loads before stores: a load does not pass a store that may be to its place)
+  const int n = p.cols - c < 8 ? static_cast<int>(p.cols - c) : 8;
+  float m[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) u[i] = i < n ? load1(p, at + i) : 0.0f;
+  if (!p.momentum) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m[i] = i < n ? p.momentum[ma + i] : 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    u[i] = 0.0f;
-    if (c + i >= p.cols) continue;
-    u[i] = load1(p, at + i);
-    if (p.momentum) {
-      float m = p.momentum[ma + i];
-      if (kNorm) p.momentum[ma + i] = m = fmaf(p.mu, m, u[i]);
-      u[i] = direction(p, u[i], m);
-    }
+    if (kNorm) m[i] = fmaf(p.mu, m[i], u[i]);
+    u[i] = direction(p, u[i], m[i]);
+    if (kNorm && i < n) p.momentum[ma + i] = m[i];
   }
 }
 
