@@ -114,8 +114,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const uint32_t crank = cluster_ctarank();
   const bool leader = crank == 0;
   const int cid = static_cast<int>(blockIdx.x) / 2, n_clusters = static_cast<int>(gridDim.x) / 2;
-  const int n_valid = p.n_valid_dev ? static_cast<int>(*p.n_valid_dev) : p.rows;
-  if (n_valid == 0) return;  // the same in every CTA, before the pair's collective allocation
   const int nkb = p.H / BK;
 
   if (threadIdx.x == 0) {
@@ -131,7 +129,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     *abort_flag = 0;
     fence_barrier_init();
   }
+  // While the row list is made: the first of W on its way into L2
+  launch_dependents();
+  if (warp == 2 && lane < S::kStages && lane < nkb && cid < p.n_tiles)
+    tma_prefetch_2d(&tm_w, lane * BK, cid * 2 * BM + static_cast<int32_t>(crank) * BM);
   cluster_sync();  // both CTAs run and their barriers exist
+  wait_for_previous();
+  const int n_valid = p.n_valid_dev ? static_cast<int>(*p.n_valid_dev) : p.rows;
+  if (n_valid == 0) return;  // the same in every CTA, before the pair's collective allocation
   if (warp == 1) {
     tmem_alloc_pair(tmem_slot, S::kTmemCols);
     tmem_relinquish_pair();
@@ -351,6 +356,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
                      float* __restrict__ lse_out, float* __restrict__ entropy, int32_t* status) {
   const int lane = threadIdx.x & 31;
   const int r = static_cast<int>(blockIdx.x) * kMergeWarps + (threadIdx.x >> 5);
+  wait_for_previous();
   const int n_valid = n_valid_dev ? static_cast<int>(*n_valid_dev) : rows;
   if (r >= n_valid) return;
   const int64_t o = static_cast<int64_t>(r) * parts;
@@ -400,6 +406,27 @@ pace_status few_clusters(int* out) {
   return PACE_OK;
 }
 
+// A launch that may start before the one ahead of it is done; the kernel waits for it itself.
+template <typename... Params, typename... Args>
+pace_status launch_early(void (*kernel)(Params...), int blocks, int threads, size_t smem,
+                         cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
+  cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, Params(args)...) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return PACE_ERR_CUDA;
+  }
+  return last_launch_status();
+}
+
 template <int N>
 pace_status launch_few(const void* hidden, const void* w_vocab, FewArgs a, const LmWs& ws,
                        float* logprob, float* lse, float* entropy, float temperature,
@@ -420,14 +447,12 @@ pace_status launch_few(const void* hidden, const void* w_vocab, FewArgs a, const
   if (clusters > a.n_tiles) clusters = a.n_tiles;
   const ProfileEvents& pe = profile_events(PACE_PROFILE_LMHEAD);
   if (pe.begin) PACE_TRY_CUDA(cudaEventRecord(pe.begin, st));
-  few_kernel<N><<<static_cast<unsigned>(2 * clusters), kThreads, Shape<N>::kSmem, st>>>(tw, th, a);
-  PACE_TRY(last_launch_status());
+  PACE_TRY(launch_early(few_kernel<N>, 2 * clusters, kThreads, Shape<N>::kSmem, st, tw, th, a));
   if (pe.end) PACE_TRY_CUDA(cudaEventRecord(pe.end, st));
-  few_merge_kernel<<<static_cast<unsigned>((a.rows + kMergeWarps - 1) / kMergeWarps),
-                     kMergeWarps * 32, 0, st>>>(
-      a.n_valid_dev, a.rows, 2 * clusters, a.V, 1.0f / temperature, a.part_m, a.part_s, a.part_t,
-      a.tgt_logit, a.targets, a.rowidx, logprob, lse, entropy, a.status);
-  return last_launch_status();
+  return launch_early(few_merge_kernel, (a.rows + kMergeWarps - 1) / kMergeWarps,
+                      kMergeWarps * 32, 0, st, a.n_valid_dev, a.rows, 2 * clusters, a.V,
+                      1.0f / temperature, a.part_m, a.part_s, a.part_t, a.tgt_logit, a.targets,
+                      a.rowidx, logprob, lse, entropy, a.status);
 }
 
 }  // namespace

@@ -691,6 +691,7 @@ __global__ void __launch_bounds__(kFewThreads)
                          long long* __restrict__ total, float* __restrict__ lp,
                          float* __restrict__ lse, float* __restrict__ entropy, AdvJob adv,
                          unsigned* counter0, unsigned* counter1, int32_t* status) {
+  launch_dependents();  // (the few-row head)
   if (static_cast<int>(blockIdx.x) >= blocks) {
     adv_block_call(adv, blockIdx.x - blocks);
     return;

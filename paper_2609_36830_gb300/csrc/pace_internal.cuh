@@ -250,6 +250,12 @@ __device__ __forceinline__ void tma_prefetch_desc(const void* desc) {
 // One box into this CTA's shared memory; its transaction bytes complete on the
 // mbarrier at shared::cluster address bar_caddr, which may belong to either CTA
 // of this CTA's pair (both CTAs of a pair feed the even CTA's barrier).
+__device__ __forceinline__ void tma_prefetch_2d(const void* desc, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(desc),
+               "r"(x), "r"(y)
+               : "memory");
+}
+
 __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const void* desc,
                                                  uint32_t bar_caddr, int32_t x, int32_t y,
                                                  uint64_t cache_hint) {
@@ -476,6 +482,15 @@ __device__ __forceinline__ uint32_t bf16x2_rn(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+
+// Programmatic dependent launches: the kernel before this one may let it start early
+// (launch_dependents); what the one before wrote is there after wait_for_previous.
+__device__ __forceinline__ void launch_dependents() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void wait_for_previous() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // The tensor cores' float32 sums drop what lies below their last place, so a sum of n
