@@ -193,6 +193,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t crank = cluster_ctarank();
   const bool leader = crank == 0;
+  launch_dependents();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < GSTAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tmem_full[b], 1);
+      mbar_init(&tmem_empty[b], 2 * 4);  // one arrival per epilogue warp of the pair
+    }
+    mbar_init(mma_done, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  cluster_sync();  // both CTAs run and their barriers exist
+  wait_for_previous();
   // The host sizes a chunk by its row capacity; the rows of it that are in the
   // loss are known only on the device (the compaction's count).  Tiles past
   // them hold zero rows: M (G, dH) or K (dW) is cut to the count rounded up to
@@ -241,20 +257,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
   };
   const int pace_rounds = max(1, kPaceSteps / nkb_all);
 
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < GSTAGES; ++s) {
-      mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 1);
-    }
-    for (int b = 0; b < 2; ++b) {
-      mbar_init(&tmem_full[b], 1);
-      mbar_init(&tmem_empty[b], 2 * 4);  // one arrival per epilogue warp of the pair
-    }
-    mbar_init(mma_done, 1);
-    *abort_flag = 0;
-    fence_barrier_init();
-  }
-  cluster_sync();  // both CTAs run and their barriers exist
   if (warp == 1) {
     tmem_alloc_pair(tmem_slot, kGTmemCols);
     tmem_relinquish_pair();
@@ -626,6 +628,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 template <bool kOut16>
 __global__ void __launch_bounds__(256)
     reduce_tail_kernel(GemmArgs p, int n_clusters) {
+  launch_dependents();
+  wait_for_previous();
   int64_t v = static_cast<int64_t>(*p.n_valid) - p.chunk_row0;
   v = v < 0 ? 0 : (v > p.M ? p.M : v);
   const int64_t m_tiles = (v + GBM - 1) / GBM;
@@ -664,6 +668,7 @@ __global__ void __launch_bounds__(256)
 
 // A bf16 copy of n float32 values (n a multiple of 8).
 __global__ void to_bf16_kernel(const float4* __restrict__ in, uint4* __restrict__ out, int64_t n) {
+  wait_for_previous();
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n / 8;
        i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
     const float4 a = in[2 * i], b = in[2 * i + 1];
@@ -930,13 +935,11 @@ pace_status launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUte
   const int64_t max_clusters = gemm_clusters();
   const int64_t grid = 2 * (items < max_clusters && !a.part ? items : max_clusters);
   a.round_ctr = round_ctr;
-  gemm_kernel<A_MN, B_MN, EPI><<<static_cast<unsigned>(grid), kGemmThreads, kGSmemBytes, st>>>(
-      ta, tb, tc, a);
-  PACE_TRY(last_launch_status());
+  PACE_TRY(launch_early(gemm_kernel<A_MN, B_MN, EPI>, static_cast<int>(grid), kGemmThreads,
+                        kGSmemBytes, st, ta, tb, tc, a));
   if ((EPI == EPI_ROWS || EPI == EPI_ROWS16) && a.part) {
-    reduce_tail_kernel<EPI == EPI_ROWS16><<<static_cast<unsigned>(sm_count() * 4), 256, 0, st>>>(
-        a, static_cast<int>(max_clusters));
-    return last_launch_status();
+    return launch_early(reduce_tail_kernel<EPI == EPI_ROWS16>, sm_count() * 4, 256, 0, st, a,
+                        static_cast<int>(max_clusters));
   }
   return PACE_OK;
 }
@@ -1214,10 +1217,9 @@ pace_status backward_call(const PaceBatch* batch, const void* hidden, const void
     ++round_ctr;
   }
   if (ws.dw) {
-    to_bf16_kernel<<<static_cast<unsigned>(sm_count() * 8), 256, 0, st>>>(
-        reinterpret_cast<const float4*>(ws.dw), static_cast<uint4*>(grad_w),
-        static_cast<int64_t>(V) * H);
-    return last_launch_status();
+    return launch_early(to_bf16_kernel, sm_count() * 8, 256, 0, st,
+                        reinterpret_cast<const float4*>(ws.dw), static_cast<uint4*>(grad_w),
+                        static_cast<int64_t>(V) * H);
   }
   return PACE_OK;
 }

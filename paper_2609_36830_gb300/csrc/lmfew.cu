@@ -406,27 +406,6 @@ pace_status few_clusters(int* out) {
   return PACE_OK;
 }
 
-// A launch that may start before the one ahead of it is done; the kernel waits for it itself.
-template <typename... Params, typename... Args>
-pace_status launch_early(void (*kernel)(Params...), int blocks, int threads, size_t smem,
-                         cudaStream_t st, const Args&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
-  cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kernel, Params(args)...) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return PACE_ERR_CUDA;
-  }
-  return last_launch_status();
-}
-
 template <int N>
 pace_status launch_few(const void* hidden, const void* w_vocab, FewArgs a, const LmWs& ws,
                        float* logprob, float* lse, float* entropy, float temperature,

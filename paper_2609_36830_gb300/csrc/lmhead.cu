@@ -427,16 +427,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
   const bool leader = crank == 0;
   const int n_clusters = static_cast<int>(gridDim.x) / CLUSTER;
   const int cid = static_cast<int>(blockIdx.x) / CLUSTER;
-  const int64_t n_valid = p.n_valid_dev ? static_cast<int64_t>(*p.n_valid_dev) : p.rows_cap;
-  const int64_t row_pairs = (n_valid + 2 * BM - 1) / (2 * BM);
-  const LmPlan plan_w = lm_plan(row_pairs, n_clusters, p.n_vtiles, p.split_pref);
-  // every CTA reads the same n_valid: the exit is uniform, and comes before the
-  // pair's collective tensor-memory allocation
-  if (row_pairs == 0) return;
-  const TailSpan span(plan_w.tail_rp > 0 ? plan_w.tail_rp : 1, n_clusters, cid);
-  Segments seg(plan_w, span, p.n_vtiles, cid, n_clusters);  // each role walks its own copy
-  const int nkb = p.H / BK;
-
+  launch_dependents();
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&full[s], CLUSTER);  // each CTA's producer arrives with its bytes
@@ -451,6 +442,17 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
     fence_barrier_init();
   }
   cluster_sync();  // both CTAs run and their barriers exist
+  wait_for_previous();
+  const int64_t n_valid = p.n_valid_dev ? static_cast<int64_t>(*p.n_valid_dev) : p.rows_cap;
+  const int64_t row_pairs = (n_valid + 2 * BM - 1) / (2 * BM);
+  const LmPlan plan_w = lm_plan(row_pairs, n_clusters, p.n_vtiles, p.split_pref);
+  // every CTA reads the same n_valid: the exit is uniform, and comes before the
+  // pair's collective tensor-memory allocation
+  if (row_pairs == 0) return;
+  const TailSpan span(plan_w.tail_rp > 0 ? plan_w.tail_rp : 1, n_clusters, cid);
+  Segments seg(plan_w, span, p.n_vtiles, cid, n_clusters);  // each role walks its own copy
+  const int nkb = p.H / BK;
+
   if (warp == 1) {
     tmem_alloc_pair(tmem_slot, kTmemCols);
     tmem_relinquish_pair();
@@ -811,6 +813,7 @@ __global__ void __launch_bounds__(kMergeThreads)
                      const float* __restrict__ part_t, const float* __restrict__ tgt_logit, const int32_t* __restrict__ targets,
                      const int32_t* __restrict__ rowidx, float* __restrict__ logprob,
                      float* __restrict__ lse_out, float* __restrict__ entropy, int32_t* status) {
+  wait_for_previous();
   const unsigned full = 0xffffffffu;
   const int64_t n_valid = n_valid_dev ? static_cast<int64_t>(*n_valid_dev) : rows_cap;
   // how the LM head dealt these rows
@@ -907,8 +910,8 @@ pace_status launch_lmhead(const LmLaunch& l, LmArgs a, cudaStream_t st) {
       am.box[j] = am.box[max_level];
   }
   a.max_level = max_level;
-  lmhead_lse_kernel<kFine, kEntropy><<<l.grid, kThreads, kSmemBytes, st>>>(am, l.tm_b, a);
-  return last_launch_status();
+  return launch_early(lmhead_lse_kernel<kFine, kEntropy>, static_cast<int>(l.grid), kThreads,
+                      kSmemBytes, st, am, l.tm_b, a);
 }
 
 template <bool kFine, bool kEntropy>
@@ -1075,11 +1078,10 @@ pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* 
   const int64_t cap = static_cast<int64_t>(sm_count()) * 8;
   if (mblocks > cap) mblocks = cap;
   const auto merge = entropy ? lse_merge_kernel<true> : lse_merge_kernel<false>;
-  merge<<<static_cast<unsigned>(mblocks), kMergeThreads, 0, st>>>(
-      rows_cap, n_valid_dev, static_cast<int>(clusters), n_vtiles, a.split_pref, V,
-      1.0f / temperature, ws.part_m, ws.part_s, ws.part_t, ws.tgt, targets, rowidx, logprob, lse,
-      entropy, status_dev);
-  return last_launch_status();
+  return launch_early(merge, static_cast<int>(mblocks), kMergeThreads, 0, st, rows_cap, n_valid_dev,
+                      static_cast<int>(clusters), n_vtiles, a.split_pref, V, 1.0f / temperature,
+                      ws.part_m, ws.part_s, ws.part_t, ws.tgt, targets, rowidx, logprob, lse,
+                      entropy, status_dev);
 }
 
 }  // namespace pace

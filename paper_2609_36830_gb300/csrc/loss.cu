@@ -655,6 +655,7 @@ __global__ void __launch_bounds__(kRowThreads)
                       int32_t* __restrict__ rowidx, long long* __restrict__ total,
                       float* __restrict__ lp, float* __restrict__ lse,
                       float* __restrict__ entropy) {
+  launch_dependents();
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int64_t warp = static_cast<int64_t>(blockIdx.x) * kRowWarps + wid;
   const int64_t w0 = warp * geom.per_warp;
@@ -691,7 +692,7 @@ __global__ void __launch_bounds__(kFewThreads)
                          long long* __restrict__ total, float* __restrict__ lp,
                          float* __restrict__ lse, float* __restrict__ entropy, AdvJob adv,
                          unsigned* counter0, unsigned* counter1, int32_t* status) {
-  launch_dependents();  // (the few-row head)
+  launch_dependents();
   if (static_cast<int>(blockIdx.x) >= blocks) {
     adv_block_call(adv, blockIdx.x - blocks);
     return;
@@ -736,6 +737,8 @@ __global__ void gather_rows_kernel(const uint4* __restrict__ hidden, int64_t row
                                    const int32_t* __restrict__ rowidx,
                                    const long long* __restrict__ n_in, int pad, int64_t rows_end,
                                    uint4* __restrict__ out) {
+  launch_dependents();
+  wait_for_previous();
   const long long m = *n_in;
   int64_t end = (m + pad - 1) / pad * pad;
   if (end > rows_end) end = rows_end;
@@ -814,10 +817,9 @@ pace_status run_gather(const void* hidden, int H, int64_t n_rows, const CompactW
   int64_t blocks = (n_rows + 7) / 8;
   const int64_t cap = static_cast<int64_t>(sm_count()) * 16;
   if (blocks > cap) blocks = cap;
-  gather_rows_kernel<<<static_cast<unsigned>(blocks), 256, 0, st>>>(
-      static_cast<const uint4*>(hidden), row_vecs, ws.rowidx, ws.total, pad, rows_end,
-      static_cast<uint4*>(out));
-  return last_launch_status();
+  return launch_early(gather_rows_kernel, static_cast<int>(blocks), 256, 0, st,
+                      static_cast<const uint4*>(hidden), row_vecs, ws.rowidx, ws.total, pad,
+                      rows_end, static_cast<uint4*>(out));
 }
 
 }  // namespace pace

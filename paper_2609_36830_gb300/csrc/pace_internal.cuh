@@ -493,6 +493,27 @@ __device__ __forceinline__ void wait_for_previous() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// A launch that may start before the one ahead of it is done; the kernel waits for it itself.
+template <typename... Params, typename... Args>
+pace_status launch_early(void (*kernel)(Params...), int blocks, int threads, size_t smem,
+                         cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
+  cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, Params(args)...) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return PACE_ERR_CUDA;
+  }
+  return last_launch_status();
+}
+
 // The tensor cores' float32 sums drop what lies below their last place, so a sum of n
 // products comes out nearer to zero than it is: by half a last place of the running sum for
 // every 16 products, which grows towards the result, or n / 16 x 2^-26 of it on average.
