@@ -935,7 +935,7 @@ pace_status launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUte
   const int64_t max_clusters = gemm_clusters();
   const int64_t grid = 2 * (items < max_clusters && !a.part ? items : max_clusters);
   a.round_ctr = round_ctr;
-  PACE_TRY(launch_early(gemm_kernel<A_MN, B_MN, EPI>, static_cast<int>(grid), kGemmThreads,
+  PACE_TRY(launch_early(gemm_kernel<A_MN, B_MN, EPI>, static_cast<unsigned>(grid), kGemmThreads,
                         kGSmemBytes, st, ta, tb, tc, a));
   if ((EPI == EPI_ROWS || EPI == EPI_ROWS16) && a.part) {
     return launch_early(reduce_tail_kernel<EPI == EPI_ROWS16>, sm_count() * 4, 256, 0, st, a,

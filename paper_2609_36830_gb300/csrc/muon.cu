@@ -909,6 +909,10 @@ __global__ void __launch_bounds__(kElemThreads, 4) direction_kernel(const UArgs 
   const int64_t step = static_cast<int64_t>(gridDim.x) * kElemThreads;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __shared__ float s_sum[kWarps];
+  if (kNorm)
+    launch_dependents();
+  else
+    wait_for_previous();  // the momentum and the sums
   int64_t v0 = static_cast<int64_t>(blockIdx.x) * kElemThreads + threadIdx.x;
   float u[kElemUnroll][8];
   direction_groups<kNorm>(p, z, v0, step, n, groups, u);
@@ -1728,8 +1732,7 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
                    static_cast<unsigned>(batch), 1);
   direction_kernel<true><<<egrid, kElemThreads, 0, st>>>(u);
   PACE_TRY(last_launch_status());
-  direction_kernel<false><<<egrid, kElemThreads, 0, st>>>(u);
-  PACE_TRY(last_launch_status());
+  PACE_TRY(launch_early(direction_kernel<false>, egrid, kElemThreads, 0, st, u));
 
   // as many pairs as the phase of most items can use (its tiles as halves)
   int64_t pairs = 2 * batch * step_tiles(n.s, n.l);

@@ -495,10 +495,10 @@ __device__ __forceinline__ void wait_for_previous() {
 
 // A launch that may start before the one ahead of it is done; the kernel waits for it itself.
 template <typename... Params, typename... Args>
-pace_status launch_early(void (*kernel)(Params...), int blocks, int threads, size_t smem,
+pace_status launch_early(void (*kernel)(Params...), dim3 blocks, int threads, size_t smem,
                          cudaStream_t st, const Args&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
+  cfg.gridDim = blocks;
   cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
