@@ -706,8 +706,8 @@ PACE_API pace_status pace_muon_update(float* weight, void* weight_bf16, const vo
                                       int32_t* status_dev, void* stream);
 
 /* Workspace of both: two copies of X and one of the s x s products in fp16, partial sums
- * and, where one side is many times the other, up to 20 MB of partial products (so a
- * long matrix may need more than a larger square one). */
+ * and, where one side is many times the other or at most 256, up to 40 MB of partial
+ * products (so a long matrix may need more than a larger square one). */
 PACE_API size_t pace_muon_workspace_size(int64_t batch, int64_t rows, int64_t cols);
 
 /* ------------------------------------------------------------------------ */

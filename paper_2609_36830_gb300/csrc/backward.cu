@@ -668,7 +668,6 @@ __global__ void __launch_bounds__(256)
 
 // A bf16 copy of n float32 values (n a multiple of 8).
 __global__ void to_bf16_kernel(const float4* __restrict__ in, uint4* __restrict__ out, int64_t n) {
-  wait_for_previous();
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n / 8;
        i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
     const float4 a = in[2 * i], b = in[2 * i + 1];
@@ -935,11 +934,12 @@ pace_status launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUte
   const int64_t max_clusters = gemm_clusters();
   const int64_t grid = 2 * (items < max_clusters && !a.part ? items : max_clusters);
   a.round_ctr = round_ctr;
-  PACE_TRY(launch_early(gemm_kernel<A_MN, B_MN, EPI>, static_cast<unsigned>(grid), kGemmThreads,
-                        kGSmemBytes, st, ta, tb, tc, a));
+  const bool early = short_product(a.M, a.N, a.K);
+  PACE_TRY(launch_early(early, gemm_kernel<A_MN, B_MN, EPI>, static_cast<unsigned>(grid),
+                        kGemmThreads, kGSmemBytes, st, ta, tb, tc, a));
   if ((EPI == EPI_ROWS || EPI == EPI_ROWS16) && a.part) {
-    return launch_early(reduce_tail_kernel<EPI == EPI_ROWS16>, sm_count() * 4, 256, 0, st, a,
-                        static_cast<int>(max_clusters));
+    return launch_early(early, reduce_tail_kernel<EPI == EPI_ROWS16>, sm_count() * 4, 256, 0, st,
+                        a, static_cast<int>(max_clusters));
   }
   return PACE_OK;
 }
@@ -1217,9 +1217,10 @@ pace_status backward_call(const PaceBatch* batch, const void* hidden, const void
     ++round_ctr;
   }
   if (ws.dw) {
-    return launch_early(to_bf16_kernel, sm_count() * 8, 256, 0, st,
-                        reinterpret_cast<const float4*>(ws.dw), static_cast<uint4*>(grad_w),
-                        static_cast<int64_t>(V) * H);
+    to_bf16_kernel<<<static_cast<unsigned>(sm_count() * 8), 256, 0, st>>>(
+        reinterpret_cast<const float4*>(ws.dw), static_cast<uint4*>(grad_w),
+        static_cast<int64_t>(V) * H);
+    return last_launch_status();
   }
   return PACE_OK;
 }

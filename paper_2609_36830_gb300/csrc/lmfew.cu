@@ -426,9 +426,9 @@ pace_status launch_few(const void* hidden, const void* w_vocab, FewArgs a, const
   if (clusters > a.n_tiles) clusters = a.n_tiles;
   const ProfileEvents& pe = profile_events(PACE_PROFILE_LMHEAD);
   if (pe.begin) PACE_TRY_CUDA(cudaEventRecord(pe.begin, st));
-  PACE_TRY(launch_early(few_kernel<N>, 2 * clusters, kThreads, Shape<N>::kSmem, st, tw, th, a));
+  PACE_TRY(launch_early(true, few_kernel<N>, 2 * clusters, kThreads, Shape<N>::kSmem, st, tw, th, a));
   if (pe.end) PACE_TRY_CUDA(cudaEventRecord(pe.end, st));
-  return launch_early(few_merge_kernel, (a.rows + kMergeWarps - 1) / kMergeWarps,
+  return launch_early(true, few_merge_kernel, (a.rows + kMergeWarps - 1) / kMergeWarps,
                       kMergeWarps * 32, 0, st, a.n_valid_dev, a.rows, 2 * clusters, a.V,
                       1.0f / temperature, a.part_m, a.part_s, a.part_t, a.tgt_logit, a.targets,
                       a.rowidx, logprob, lse, entropy, a.status);

@@ -910,8 +910,8 @@ pace_status launch_lmhead(const LmLaunch& l, LmArgs a, cudaStream_t st) {
       am.box[j] = am.box[max_level];
   }
   a.max_level = max_level;
-  return launch_early(lmhead_lse_kernel<kFine, kEntropy>, l.grid, kThreads,
-                      kSmemBytes, st, am, l.tm_b, a);
+  return launch_early(short_product(l.n_rows, a.V, l.H), lmhead_lse_kernel<kFine, kEntropy>,
+                      l.grid, kThreads, kSmemBytes, st, am, l.tm_b, a);
 }
 
 template <bool kFine, bool kEntropy>
@@ -1078,7 +1078,8 @@ pace_status run_logprob(const PaceBatch* batch, const void* hidden, const void* 
   const int64_t cap = static_cast<int64_t>(sm_count()) * 8;
   if (mblocks > cap) mblocks = cap;
   const auto merge = entropy ? lse_merge_kernel<true> : lse_merge_kernel<false>;
-  return launch_early(merge, static_cast<unsigned>(mblocks), kMergeThreads, 0, st, rows_cap, n_valid_dev,
+  return launch_early(short_product(n_rows, V, H), merge, static_cast<unsigned>(mblocks),
+                      kMergeThreads, 0, st, rows_cap, n_valid_dev,
                       static_cast<int>(clusters), n_vtiles, a.split_pref, V, 1.0f / temperature,
                       ws.part_m, ws.part_s, ws.part_t, ws.tgt, targets, rowidx, logprob, lse,
                       entropy, status_dev);

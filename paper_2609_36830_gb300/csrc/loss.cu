@@ -817,7 +817,7 @@ pace_status run_gather(const void* hidden, int H, int64_t n_rows, const CompactW
   int64_t blocks = (n_rows + 7) / 8;
   const int64_t cap = static_cast<int64_t>(sm_count()) * 16;
   if (blocks > cap) blocks = cap;
-  return launch_early(gather_rows_kernel, static_cast<unsigned>(blocks), 256, 0, st,
+  return launch_early(true, gather_rows_kernel, static_cast<unsigned>(blocks), 256, 0, st,
                       static_cast<const uint4*>(hidden), row_vecs, ws.rowidx, ws.total, pad,
                       rows_end, static_cast<uint4*>(out));
 }

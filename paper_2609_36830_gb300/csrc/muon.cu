@@ -148,8 +148,8 @@ __host__ __device__ inline Deal deal_tiles(int64_t tiles, int n_clusters) {
 // Parts along l for the tiles of X X^T.  Few tiles of a long X would leave most pairs idle
 // for l / 64 K steps of 0.25 us; in n parts they take an n-th of that and another phase, some
 // 5 us, which reads n parts one after the other, so n is at most the root of the K steps.
-// (256 x 14,336: 365 us in one part, 177 in 14, 650 in 56; 100 x 5,000 188 in one and 144 in
-// 8.)  From kMaxClusters, so that the workspace does not depend on the device.
+// (300 x 14,336: 366 us in one part, 187 in 14; 4 of 200 x 6,200 228 and 174; 56 parts are
+// slower than one.)  From kMaxClusters, so that the workspace does not depend on the device.
 __host__ __device__ inline int gram_split(int64_t tiles, int64_t l) {
   const int64_t nkb = (l + BK - 1) / BK;
   int64_t n = 1;
@@ -980,12 +980,13 @@ __global__ void __launch_bounds__(kElemThreads, 4) direction_kernel(const UArgs 
 // ------------------------------------------------- matrices whose shorter side is up to 256
 
 // One CTA pair does everything for a matrix of at most 256 x 256, in shared memory and
-// without a grid barrier: norm, all products, result.  (The phases of
+// without a grid barrier: norm, all products, result, 62 us for 256 x 256.  (The phases of
 // newton_schulz_kernel spend 4-5 us each in barrier, loads and stores whatever the size.)
 // A longer X is cut into slices of 256 columns, a pair each: C X needs no other slice, and
 // X X^T is the sum of the slices' products.  The pairs of a matrix meet twice a step: every
 // pair leaves its product in float32, each CTA adds up its share of them, in the order of the
-// slices, and every CTA reads the rows of A that it needs.
+// slices, and every CTA reads the rows of A that it needs.  (256 x 2,048 103 us, 100 x 5,000 91,
+// 256 x 14,336 115; newton_schulz_kernel 138, 150 and 185.)
 // X is s x l with s <= l, so a tall U is transposed as it is read.  Operands lie in the
 // layouts that the TMA would build (128-byte swizzle), 64 KB each in a CTA:
 //   rows     the CTA's 128 rows of X, and of C: [K block][128 rows][64], K-major.  They are
@@ -1517,16 +1518,18 @@ void carve_muon_ws(Carver& cv, int64_t batch, int64_t rows, int64_t cols, MuonWs
   w->ctr = cv.take<unsigned>(static_cast<size_t>(batch > 0 && batch < kMaxClusters ? batch : 1));
   const int64_t tiles = batch * sym_tiles(s);
   w->split = tiles > 0 ? gram_split(tiles, rows < cols ? cols : rows) : 1;
-  w->part = w->split > 1 ? cv.take<float>(static_cast<size_t>(tiles) * w->split * TM * TM) : nullptr;
+  size_t parts = w->split > 1 ? static_cast<size_t>(tiles) * w->split * TM * TM : 0;
   w->slices = slice_count(batch, s, rows < cols ? cols : rows);
-  w->slice_part = w->slice_sum = nullptr;
+  w->slice_sum = nullptr;
   w->direct = 0;
   if (w->slices > 1) {
     const size_t pairs = static_cast<size_t>(batch) * w->slices, nb = (s + 31) / 32;
     w->direct = add_directly(w->slices, s);
-    w->slice_part = cv.take<float>((1 + w->direct) * pairs * nb * nb * 1024);
+    const size_t slice_parts = (1 + w->direct) * pairs * nb * nb * 1024;
+    if (slice_parts > parts) parts = slice_parts;
     w->slice_sum = cv.take<float>(pairs);
   }
+  w->part = w->slice_part = parts ? cv.take<float>(parts) : nullptr;  // (one or the other runs)
 }
 
 // The largest |a x + b x^3 + c x^5| over 0 <= x <= r.
@@ -1732,7 +1735,7 @@ pace_status run_newton_schulz(UArgs u, NsArgs n, int64_t batch, const PaceMuonPa
                    static_cast<unsigned>(batch), 1);
   direction_kernel<true><<<egrid, kElemThreads, 0, st>>>(u);
   PACE_TRY(last_launch_status());
-  PACE_TRY(launch_early(direction_kernel<false>, egrid, kElemThreads, 0, st, u));
+  PACE_TRY(launch_early(true, direction_kernel<false>, egrid, kElemThreads, 0, st, u));
 
   // as many pairs as the phase of most items can use (its tiles as halves)
   int64_t pairs = 2 * batch * step_tiles(n.s, n.l);

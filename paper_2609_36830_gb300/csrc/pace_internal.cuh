@@ -493,10 +493,15 @@ __device__ __forceinline__ void wait_for_previous() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// A launch that may start before the one ahead of it is done; the kernel waits for it itself.
+// A launch that may start before the one ahead of it is done (`early`); the kernel waits for
+// it itself.  It saves 2 us a launch, but blocks that wait beside a long launch slow it down
+// (a 37,000-row step of the H 3,584 head 88 -> 90-93 ms, 21,000 rows backward 40.7 -> 41.3), so
+// calls are launched so that are short: products of up to kEarlyFlops, some 200 us.
+constexpr double kEarlyFlops = 3e11;
+inline bool short_product(double m, double n, double k) { return 2.0 * m * n * k <= kEarlyFlops; }
 template <typename... Params, typename... Args>
-pace_status launch_early(void (*kernel)(Params...), dim3 blocks, int threads, size_t smem,
-                         cudaStream_t st, const Args&... args) {
+pace_status launch_early(bool early, void (*kernel)(Params...), dim3 blocks, int threads,
+                         size_t smem, cudaStream_t st, const Args&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = blocks;
   cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
@@ -506,7 +511,7 @@ pace_status launch_early(void (*kernel)(Params...), dim3 blocks, int threads, si
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = early ? 1 : 0;
   if (cudaLaunchKernelEx(&cfg, kernel, Params(args)...) != cudaSuccess) {
     (void)cudaGetLastError();
     return PACE_ERR_CUDA;
