@@ -88,6 +88,11 @@ constexpr int kThreads = 192;
 constexpr uint32_t kStageA = BM * BK * 2;       // 16 KB: this CTA's 128 hidden rows
 constexpr uint32_t kStageB = BN / CLUSTER * BK * 2;  // 16 KB: this CTA's half of the vocabulary tile
 constexpr uint32_t kTmemCols = 2 * BN;          // two fp32 accumulators of 256 columns
+// Inside an item of the rounds the clusters meet about every kPaceSteps K steps (0.7 ms).
+// Meeting at items only, every few ms, they drift apart by more than L2 holds: a 37,000-row step
+// of H 3,584 (2.8 ms an item) read 57 GB of DRAM and took 91 ms, 87 with the meetings; 512
+// steps the same.  In the tail, which all walk together, they gain nothing.
+constexpr int kPaceSteps = 2048;
 constexpr uint32_t kIdesc = idesc_bf16_f32(CLUSTER * BM, BN);
 // Shared memory: the hidden tiles, each with a 16 KB spill region before and
 // after it (shared by neighbours: spill | A0 | spill | A1 | ... | A3 | spill),
@@ -512,19 +517,30 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
       }
       __syncwarp();  // row_src and piece are rewritten by the next plan
     };
+    const int pace_tiles = max(1, kPaceSteps / nkb);
+    const unsigned meets = 1u + static_cast<unsigned>((plan_w.tiles_per_split - 1) / pace_tiles);
     for (; ok && seg.load(); ++round) {
       BlockLoads b0, b1;
+      unsigned met = 0;  // of this round
       plan_block(seg.rp, b0);
       b1 = b0;
       if (seg.two()) plan_block(seg.rp + 1, b1);
       // every round is full, so round k (or the tail) starts once all clusters
-      // issued their round k-1 loads (the even CTA paces the pair)
+      // issued their round k-1 loads (the even CTA paces the pair); `meets` arrivals a round
       if (leader && lane == 0 && round > 0 && p.round_ctr)
-        wait_round(p.round_ctr, round * static_cast<unsigned>(n_clusters));
+        wait_round(p.round_ctr, round * meets * static_cast<unsigned>(n_clusters));
       __syncwarp();
       for (int t = seg.tile0; t < seg.tile1 && ok; ++t) {
         const int which = seg.tile();
         if (which < 0) continue;
+        if (!seg.is_tail && t > seg.tile0 && (t - seg.tile0) % pace_tiles == 0) {
+          ++met;
+          if (leader && lane == 0 && p.round_ctr) {
+            atomicAdd(p.round_ctr, 1u);
+            wait_round(p.round_ctr, (round * meets + met) * static_cast<unsigned>(n_clusters));
+          }
+          __syncwarp();
+        }
         const BlockLoads bl = which ? b1 : b0;
         const int issuers = bl.scattered ? 1 : bl.n + 1;
         const int32_t nb = t * BN + static_cast<int32_t>(crank) * (BN / CLUSTER);
@@ -562,7 +578,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(kThreads, 1)
                              bl.g4[1], bl.g4[2], bl.g4[3], pol);
         }
       }
-      if (leader && lane == 0 && ok && p.round_ctr) atomicAdd(p.round_ctr, 1u);
+      if (leader && lane == 0 && ok && p.round_ctr) atomicAdd(p.round_ctr, meets - met);
     }
     if (lane == 0) {
       if (!ok) give_up();
