@@ -413,7 +413,8 @@ pace_status launch_few(const void* hidden, const void* w_vocab, FewArgs a, const
   CUtensorMap tw, th;
   PACE_TRY(encode_bf16_2d(&tw, w_vocab, a.V, a.H, a.H, BK, BM));
   // Listed rows: up to 32, one row a box and four boxes a gather.  More gathers than four a
-  // stage are slower than the stage's 16 KB of W (H 2,048, V 151,936, us a call: 32 rows 112,
+  // stage are slower than the stage's 16 KB of W (H 2,048, V 151,936, us a call before its
+  // launches overlapped, 5 less since: 32 rows 112,
   // 64 rows 144, 128 rows 215), so more rows are copied first (64 rows 116, 128 rows 120).
   a.gather = a.rowidx && N <= 32 ? 1 : 0;
   if (a.rowidx && !a.gather) {

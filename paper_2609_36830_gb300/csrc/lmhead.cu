@@ -49,7 +49,7 @@
 // same number of tiles, give or take one, and all of them walk the vocabulary
 // together.  Each CTA writes one (max, sum) pair per row and split (rounds) or per
 // row and cluster that shares the row (tail).  A soft
-// barrier at item boundaries (wait_round) keeps the clusters of a split
+// barrier at item boundaries and inside items (wait_round) keeps the clusters of a split
 // together, so each vocabulary tile is fetched from DRAM about once per round:
 // left alone, the clusters' small speed differences add up over the hundreds
 // of rounds of a long launch, the leaders fetch tiles from DRAM that the
