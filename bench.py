@@ -47,16 +47,16 @@ PREFIX_WORKLOAD = "math7b"  # prefix rescoring and the backward are timed on the
 # DRAM bytes (read + written) per row in the loss of the LM-head kernel (rows read by index),
 # by (workload, vocabulary splits), from one-pass ncu captures (dram__bytes_read.sum +
 # dram__bytes_write.sum) of the current kernel on the MoE-shaped head.  4 splits: one wave
-# of 19,456 rows, 2.589991 GB read + 4.27 MB written; every round of items reads the
+# of 19,456 rows, 2.58 GB read + 4.04 MB written; every round of items reads the
 # vocabulary once, so the bytes grow with the rows and the wave's figure per row is scaled by
 # the launch's rows.  2 splits: a single wave is not proportional to a long launch (the
 # clusters of a split drift apart over it), so the figure is one full 3,958,414-row launch,
-# 298.063 GB read + 129.3 MB written.  Emptied whenever the kernel changes, until it is
+# 287.36 GB read + 129.76 MB written.  Emptied whenever the kernel changes, until it is
 # captured again.  The tag reduction's per tag: 219.96 MB read + 3.12 MB written for the
 # 54.93 M tags of the 16k sweep pool (the atomic-free kernel; its reads equal the algorithmic
 # bytes, so the figure per tag carries to the larger pools).
-LMHEAD_DRAM_BYTES_PER_ROW = {("moe", 4): (2589990656 + 4268800) / 19456,
-                             ("moe", 2): (298063478784 + 129295872) / 3958414}
+LMHEAD_DRAM_BYTES_PER_ROW = {("moe", 4): (2.58e9 + 4.04e6) / 19456,
+                             ("moe", 2): (287.36e9 + 129.76e6) / 3958414}
 TAG_REDUCE_DRAM_BYTES_PER_TAG = (219963904 + 3123712) / 54929421
 SWEEP_N = 1048576
 SWEEP_SIZES = (1024, 16384, 131072, SWEEP_N)
