@@ -207,6 +207,44 @@ def test_other_stream_and_graph():
         assert torch.equal(a, c)
 
 
+@pytest.mark.parametrize("rows,H,V", [(9, 256, 3000), (60, 512, 3000), (150, 256, 3000),
+                                      (700, 128, 9000)])
+def test_calls_in_a_row_on_one_workspace(rows, H, V):
+    """Short calls' launches overlap: calls in a row, with inputs and row lists in turn, give
+    the bits of calls one by one, outside a graph and in one."""
+    sets = [make(rows, H, V, keep, seed) for keep, seed in ((0.6, 1), (0.9, 2), (1.0, 3))]
+    ws = pace.workspace(pace.token_logprob_entropy_workspace_size(rows, 1, H, V), DEV)
+    wsb = pace.workspace(pace.token_logprob_entropy_backward_workspace_size(rows, 1, H, V), DEV)
+
+    def call(s, ws=None, wsb=None):
+        g, h, w, y, b, inn = s
+        lp, lse, ent = pace.token_logprob_entropy(b, h, w, y, ws=ws)
+        d = torch.linspace(-1, 1, rows, device=DEV) / rows
+        return (lp, lse, ent) + pace.token_logprob_entropy_backward(
+            b, h, w, y, lse, d, entropy=ent, dentropy=d * 0.1, ws=wsb)
+
+    want = []
+    for s in sets:
+        want.append(call(s))
+        torch.cuda.synchronize()
+
+    def check(got):
+        torch.cuda.synchronize()
+        for i, outs in enumerate(got):
+            for a, b in zip(outs, want[i % 3]):
+                assert torch.equal(a, b)
+    check([call(sets[i % 3], ws, wsb) for i in range(12)])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = [call(sets[i % 3], ws, wsb) for i in range(6)]
+    for _ in range(3):
+        for outs in got:
+            for a in outs:
+                a.zero_()
+        graph.replay()
+        check(got)
+
+
 def test_refusals():
     _, h, w, y, b, _ = make(4, 64, 300)
     x = torch.zeros(4, device=DEV)
